@@ -630,6 +630,130 @@ costa_status costa_phase_timing(int enable);
  * or if the last timed call had no tiles. */
 costa_status costa_phase_times(double *ms, int *nphases);
 
+/* ---- Low-bit matrices: microscaled storage, products and gradients ----------
+ *
+ * Forms of a matrix with fewer bits than its dense one, for what reads it next:
+ * 4-bit codes that a product reads, and 8-bit codes as the checkpoint of an
+ * activation that a backward pass reads.  They apply to one block of a layout
+ * (a rank's panel after a costa_transform, say) or to any strided matrix.  The
+ * paper has no counterpart; the formats are those of the OCP Microscaling
+ * specification v1.0 (MXFP4, MXINT8): each run of 32 elements of a row, a
+ * block, shares a power-of-two scale 2^E, kept as the byte E + 127 (255: NaN).
+ *  E2M1 - sign, 2 exponent bits, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *  I8   - an integer q in -127 .. 127 that stands for q / 64.
+ * Quantisation of a block: E = floor(log2(largest magnitude)) less 2 for E2M1,
+ * clamped to -127 .. 127 (-127 for a block of zeros); each element x 2^-E is
+ * rounded to the nearest of the format, ties to the even code, saturating at
+ * the largest.  A block that holds a NaN or an infinity gets scale 255 and
+ * zero codes: all its elements then stand for NaN.
+ *
+ * Beside the conventions at the top, these calls share:
+ *  - Streams: each call only enqueues kernels on `stream` and keeps nothing
+ *    between calls, so it may be captured in a CUDA graph.  None needs a plan
+ *    or a workspace.
+ *  - Rounding: sums and activations are evaluated in 32 bits and rounded once
+ *    to the output's type.  Repeated calls give the same bits.
+ *  - Empty matrices are allowed (rows or columns 0; null pointers then).
+ *  - Storage: memory that the current device can address, as for costa_block;
+ *    first and last byte of each matrix are checked (COSTA_ERR_LAYOUT). */
+
+/* Element types of dense matrices. */
+typedef enum { COSTA_MX_F32 = 0, COSTA_MX_BF16 = 1 } costa_mx_type;
+
+/* Formats of codes. */
+typedef enum { COSTA_MX_E2M1 = 0, COSTA_MX_I8 = 1 } costa_mx_format;
+
+/* Activations: x / (1 + e^-x); x (1 + erf(x / sqrt(2))) / 2; max(x, 0)
+ * (NaN stays NaN; its derivative at 0 is 0). */
+typedef enum { COSTA_MX_SILU = 0, COSTA_MX_GELU = 1, COSTA_MX_RELU = 2 } costa_mx_act;
+
+/* A dense matrix in row-major order: element (i, j) at ptr + (i * ld + j)
+ * elements; ptr aligned to the element size, ld >= cols.  A column-major block
+ * (the default order of layouts) is the row-major storage of its transpose.
+ * Extents below 2^31 - 256, ld below 2^38. */
+typedef struct {
+    void *ptr;
+    int64_t rows, cols, ld;
+    int32_t type;     /* costa_mx_type */
+    int32_t reserved; /* must be 0     */
+} costa_mx_dense;
+
+/* A matrix of codes with blocks of 32 along its rows.  Row i of the codes is
+ * at codes + i * ld bytes; ld is a multiple of 16; both pointers are 16-byte
+ * aligned.  With b = ceil(cols / 32) blocks to a row:
+ *  E2M1 - two elements to a byte, the first in the low half; ld >= 16 b.  The
+ *         scales lie in tiles of 128 rows x 4 blocks, 512 bytes each (the order
+ *         in which the tensor cores take them), the tiles of one band of rows
+ *         together: block j of row i is byte (i % 32) * 16 + (i % 128 / 32) * 4
+ *         + j % 4 of tile (i / 128) * ceil(b / 4) + j / 4.
+ *  I8   - one element to a byte; ld >= 32 b.  The scale of block j of row i is
+ *         byte i * 8 ceil(b / 8) + j.
+ * Elements past cols in the last block are 0, and so are E2M1's scale bytes
+ * past b in its last tile (other calls rely on both; the quantising calls
+ * write them); bytes past those, and the scales of rows past the last, may
+ * hold anything. */
+typedef struct {
+    void *codes, *scales;
+    int64_t rows, cols, ld;
+    int32_t format;   /* costa_mx_format */
+    int32_t reserved; /* must be 0       */
+} costa_mx_matrix;
+
+/* Storage that a matrix of codes needs: the least ld, the bytes of rows * ld
+ * codes and the bytes of scales.  Any of the outputs may be NULL.
+ * Errors: INVALID_ARG. */
+costa_status costa_mx_sizes(costa_mx_format format, int64_t rows, int64_t cols, int64_t *ld,
+                            int64_t *code_bytes, int64_t *scale_bytes);
+
+/* Q = codes of op(X): blocks run along X's rows for COSTA_OP_N and along its
+ * columns for COSTA_OP_T (or C).  Errors: INVALID_ARG, SHAPE (extents of Q and
+ * op(X) differ), LAYOUT, CUDA. */
+costa_status costa_mx_quantize(const costa_mx_dense *X, costa_op op, const costa_mx_matrix *Q, void *stream);
+
+/* QN = codes of X and QT = codes of its transpose, of one format, from one
+ * pass over X (a gradient dY: QN for dX = dY W, QT for dW = dY^T X).  The same
+ * bits as two calls of costa_mx_quantize.  Errors as there. */
+costa_status costa_mx_quantize_both(const costa_mx_dense *X, const costa_mx_matrix *QN,
+                                    const costa_mx_matrix *QT, void *stream);
+
+/* Y = the values that Q stands for, rounded to Y's type (every code of a
+ * quantised matrix is exact in either).  Errors as above. */
+costa_status costa_mx_dequantize(const costa_mx_matrix *Q, const costa_mx_dense *Y, void *stream);
+
+/* C = alpha * A B^T + beta * C, A (m x k) and B (n x k) in E2M1: the product of
+ * a layer with weights B (C = X W^T), and with operands quantised by op T the
+ * products of its backward pass.  Sums in 32 bits; C f32 or bf16; with beta ==
+ * 0 C is not read; k == 0 gives beta * C.  Products and sums beyond the f32
+ * range overflow.  Errors: INVALID_ARG, SHAPE, DTYPE (a format other than
+ * E2M1), LAYOUT, CUDA. */
+costa_status costa_mx_product(const costa_mx_matrix *A, const costa_mx_matrix *B, float alpha, float beta,
+                              const costa_mx_dense *C, void *stream);
+
+/* Y = act(X), or act(X) * G element by element where G is not NULL, and the
+ * checkpoints QX and QG of X and G in I8 (what costa_mx_quantize with op N
+ * gives), in one pass.  X, G and Y have one type.  QG is NULL where G is.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, LAYOUT, CUDA. */
+costa_status costa_mx_act_forward(costa_mx_act act, const costa_mx_dense *X, const costa_mx_dense *G,
+                                  const costa_mx_dense *Y, const costa_mx_matrix *QX,
+                                  const costa_mx_matrix *QG, void *stream);
+
+/* The gradients of costa_mx_act_forward from its checkpoints: with x and g the
+ * values that QX and QG stand for, dX = dY * g * act'(x) and dG = dY * act(x),
+ * or dX = dY * act'(x) where QG and dG are NULL.  dY, dX and dG have one type.
+ * Errors as there. */
+costa_status costa_mx_act_backward(costa_mx_act act, const costa_mx_matrix *QX, const costa_mx_matrix *QG,
+                                   const costa_mx_dense *dY, const costa_mx_dense *dX,
+                                   const costa_mx_dense *dG, void *stream);
+
+/* dW = alpha * dY^T X + beta * dW, the gradient of the weights of Y = X W^T
+ * from the checkpoint QX of X (m x k, I8): dY (m x n) f32 or bf16, dW (n x k)
+ * f32 or bf16.  The products of dY's elements with the checkpoint's values are
+ * exact, for f32 dY too (of magnitude 2^-109 or more; bits below 2^-133 are
+ * dropped), and are summed in 32 bits.  With beta == 0 dW is not read; m == 0 gives beta * dW.  Errors: INVALID_ARG, SHAPE, DTYPE (a format
+ * other than I8), LAYOUT, CUDA. */
+costa_status costa_mx_weight_grad(const costa_mx_dense *dY, const costa_mx_matrix *QX, float alpha,
+                                  float beta, const costa_mx_dense *dW, void *stream);
+
 /* ABI version of this header (1). */
 int costa_abi_version(void);
 

@@ -26,6 +26,9 @@ DTYPES = {"f32": 0, "f64": 1, "c64": 2, "c128": 3}
 OPS = {"N": 0, "T": 1, "C": 2}
 MODES = {"direct": 0, "message": 1}
 ORDERS = {"C": 0, "R": 1}
+MX_TYPES = {"f32": 0, "bf16": 1}
+MX_FORMATS = {"e2m1": 0, "i8": 1}
+MX_ACTS = {"silu": 0, "gelu": 1, "relu": 2}
 _SCALAR_NP = {"f32": np.float32, "f64": np.float64, "c64": np.complex64, "c128": np.complex128}
 
 
@@ -61,7 +64,7 @@ def _load():
         raise ImportError(f"COSTA CUDA library not built ({_LIB_PATH}); "
                           "run paper_2106_06601_gb300.build.build()")
     lib = ctypes.CDLL(_LIB_PATH)
-    P, I, I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+    P, I, I64, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
     sigs = {
         "costa_layout_create": [P, I, I, I, P, I, P, P, P],
         "costa_layout_create_block_cyclic": [P, I, I64, I64, I64, I64, I, I, ctypes.c_char, P, P, P],
@@ -104,6 +107,14 @@ def _load():
         "costa_debug_exchange": [P, P, I, I, P, I, ctypes.c_uint64, ctypes.c_uint64, I, P, I64, P, P],
         "costa_debug_tma": [P, P, I, P],
         "costa_debug_fxdot": [I, I64, P, P, P, P],
+        "costa_mx_sizes": [I, I64, I64, P, P, P],
+        "costa_mx_quantize": [P, I, P, P],
+        "costa_mx_quantize_both": [P, P, P, P],
+        "costa_mx_dequantize": [P, P, P],
+        "costa_mx_product": [P, P, F, F, P, P],
+        "costa_mx_act_forward": [I, P, P, P, P, P, P],
+        "costa_mx_act_backward": [I, P, P, P, P, P, P],
+        "costa_mx_weight_grad": [P, P, F, F, P, P],
     }
     for name, args in sigs.items():
         f = getattr(lib, name)
@@ -699,3 +710,70 @@ def costa_debug_tiles(A: Layout, B: Layout, op: str) -> np.ndarray:
     _check(_lib.costa_debug_tiles(A.handle, B.handle, OPS[op], out.ctypes.data, cnt.value,
                                   ctypes.byref(cnt)))
     return out[:cnt.value]
+
+
+# ---- low-bit matrices ----
+#
+# A dense matrix and a matrix of codes are C structs packed as bytes, which the
+# calls below take as they are (0.3 us each on the Grace host).
+
+_MX_DENSE = struct.Struct("=Qqqqii")
+_MX_MATRIX = struct.Struct("=QQqqqii")
+
+
+def costa_mx_dense(dtype: str, rows: int, cols: int, ptr: int, ld: int) -> bytes:
+    """A costa_mx_dense: a row-major matrix of "f32" or "bf16" at device address
+    `ptr`, `ld` elements from row to row."""
+    return _MX_DENSE.pack(ptr, rows, cols, ld, MX_TYPES[dtype], 0)
+
+
+def costa_mx_matrix(fmt: str, rows: int, cols: int, codes_ptr: int, scales_ptr: int, ld: int) -> bytes:
+    """A costa_mx_matrix: codes of format "e2m1" or "i8" at device address
+    `codes_ptr`, `ld` bytes from row to row, and their scales."""
+    return _MX_MATRIX.pack(codes_ptr, scales_ptr, rows, cols, ld, MX_FORMATS[fmt], 0)
+
+
+def costa_mx_sizes(fmt: str, rows: int, cols: int):
+    """(least ld, bytes of codes, bytes of scales) of a matrix of codes."""
+    out = (ctypes.c_int64 * 3)()
+    at = ctypes.addressof(out)
+    _check(_lib.costa_mx_sizes(MX_FORMATS[fmt], rows, cols, at, at + 8, at + 16))
+    return tuple(out)
+
+
+def costa_mx_quantize(X: bytes, op: str, Q: bytes, stream: int = 0) -> None:
+    """Q = codes of op(X)."""
+    _check(_lib.costa_mx_quantize(X, OPS[op], Q, stream))
+
+
+def costa_mx_quantize_both(X: bytes, QN: bytes, QT: bytes, stream: int = 0) -> None:
+    """QN = codes of X, QT = codes of its transpose, from one pass over X."""
+    _check(_lib.costa_mx_quantize_both(X, QN, QT, stream))
+
+
+def costa_mx_dequantize(Q: bytes, Y: bytes, stream: int = 0) -> None:
+    """Y = the values that Q stands for."""
+    _check(_lib.costa_mx_dequantize(Q, Y, stream))
+
+
+def costa_mx_product(A: bytes, B: bytes, C: bytes, alpha: float = 1.0, beta: float = 0.0, stream: int = 0) -> None:
+    """C = alpha * A B^T + beta * C, A and B in "e2m1"."""
+    _check(_lib.costa_mx_product(A, B, alpha, beta, C, stream))
+
+
+def costa_mx_act_forward(act: str, X: bytes, G: bytes | None, Y: bytes, QX: bytes, QG: bytes | None,
+                         stream: int = 0) -> None:
+    """Y = act(X) (times G); QX (and QG): their checkpoints in "i8"."""
+    _check(_lib.costa_mx_act_forward(MX_ACTS[act], X, G, Y, QX, QG, stream))
+
+
+def costa_mx_act_backward(act: str, QX: bytes, QG: bytes | None, dY: bytes, dX: bytes, dG: bytes | None,
+                          stream: int = 0) -> None:
+    """dX (and dG) of costa_mx_act_forward from its checkpoints and dY."""
+    _check(_lib.costa_mx_act_backward(MX_ACTS[act], QX, QG, dY, dX, dG, stream))
+
+
+def costa_mx_weight_grad(dY: bytes, QX: bytes, dW: bytes, alpha: float = 1.0, beta: float = 0.0,
+                         stream: int = 0) -> None:
+    """dW = alpha * dY^T X + beta * dW with X from its "i8" checkpoint QX."""
+    _check(_lib.costa_mx_weight_grad(dY, QX, alpha, beta, dW, stream))

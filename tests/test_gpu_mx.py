@@ -1,0 +1,465 @@
+"""Low-bit matrices on the GPU against their definitions in 64 bits: codes and
+scales bit for bit; products, activations and gradients within bounds that
+follow from 32-bit sums and one rounding; nothing written outside the outputs."""
+import numpy as np
+import pytest
+
+from tests import _mx
+
+torch = pytest.importorskip("torch")
+costa = pytest.importorskip("paper_2106_06601_gb300")
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+EPS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -9}  # half a unit in the last place, relative
+GUARD = 0xA5
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+class Dense:
+    """A row-major matrix in a buffer with `shift` elements before it and `pad`
+    after each row; every other byte is a guard that has to stay."""
+
+    def __init__(self, rows, cols, dtype, values=None, pad=0, shift=0):
+        self.rows, self.cols, self.dtype, self.ld, self.shift = rows, cols, dtype, cols + pad, shift
+        n = shift + rows * self.ld + 16
+        es = 4 if dtype == "f32" else 2
+        raw = torch.full((n * es,), GUARD, dtype=torch.uint8, device="cuda")
+        self.flat = raw.view(TORCH[dtype])
+        self.view = torch.as_strided(self.flat, (rows, cols), (self.ld, 1), shift)
+        if values is not None:
+            self.view.copy_(torch.from_numpy(np.ascontiguousarray(values)).to("cuda"))
+        self.before = raw.clone()
+
+    @property
+    def c(self):
+        return costa.costa_mx_dense(self.dtype, self.rows, self.cols, self.view.data_ptr(), self.ld)
+
+    def numpy(self):
+        """The values as float64, after a look at the guards."""
+        kept = self.before.view(TORCH[self.dtype]).clone()
+        torch.as_strided(kept, (self.rows, self.cols), (self.ld, 1), self.shift).copy_(self.view)
+        assert torch.equal(kept.view(torch.uint8), self.flat.view(torch.uint8)), "written outside the matrix"
+        return self.view.double().cpu().numpy()
+
+
+class Codes:
+    def __init__(self, fmt, rows, cols, pad=0, packed=None):
+        self.fmt, self.rows, self.cols = fmt, rows, cols
+        least, _, ns = _mx.sizes(fmt, rows, cols)
+        self.ld = least + pad
+        if packed is None:
+            self.codes = torch.full((rows * self.ld + 32,), GUARD, dtype=torch.uint8, device="cuda")
+            self.scales = torch.full((ns + 32,), GUARD, dtype=torch.uint8, device="cuda")
+        else:
+            self.codes, self.scales = (torch.from_numpy(p.reshape(-1).copy()).to("cuda") for p in packed)
+
+    @property
+    def c(self):
+        return costa.costa_mx_matrix(self.fmt, self.rows, self.cols, self.codes.data_ptr(), self.scales.data_ptr(),
+                                     self.ld)
+
+    def check(self, x):
+        """The codes of x, and guards elsewhere."""
+        want = _mx.pack(self.fmt, *_mx.quantize(self.fmt, x), self.cols, self.ld, fill=GUARD)
+        codes, scales = self.codes.cpu().numpy(), self.scales.cpu().numpy()
+        n = self.rows * self.ld
+        assert np.array_equal(scales[:-32], want[1])
+        assert np.array_equal(codes[:n].reshape(self.rows, self.ld), want[0])
+        assert (codes[n:] == GUARD).all() and (scales[-32:] == GUARD).all()
+
+
+def matrix(rng, rows, cols, dtype, scale=1.0):
+    """Values of several magnitudes, rows and blocks of zeros among them."""
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-6, 7, (rows, cols)))
+    x *= np.where(rng.random((rows, 1)) < 0.1, 0.0, scale)
+    x[:, cols // 2:cols // 2 + 32][rng.random((rows, x[:, cols // 2:cols // 2 + 32].shape[1])) < 0.5] = 0.0
+    x = x.astype(np.float32)
+    return _mx.bf16(x) if dtype == "bf16" else x
+
+
+def codes_of(fmt, x, pad=0):
+    """x's codes made by the definition, and their values."""
+    packed = _mx.pack(fmt, *_mx.quantize(fmt, x), x.shape[1], _mx.sizes(fmt, *x.shape)[0] + pad, fill=GUARD)
+    return Codes(fmt, *x.shape, pad=pad, packed=packed), _mx.rounded(fmt, x)
+
+
+def close(got, want, tol):
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = np.isnan(want) | (np.abs(got - want) <= tol) | (got == want)
+    if not ok.all():
+        bad = np.argwhere(~ok)
+        i = tuple(bad[0])
+        raise AssertionError(f"{len(bad)} of {ok.size} off, first {i}: {got[i]} for {want[i]}, allowed {tol[i]}")
+
+
+SHAPES = [(1, 1), (1, 32), (1, 4096), (2, 33), (5, 8), (31, 31), (33, 64), (64, 96), (127, 129), (128, 128),
+          (256, 64), (257, 65), (300, 1000), (1000, 300), (40, 2056)]
+
+
+@pytest.mark.parametrize("rows, cols", SHAPES)
+@pytest.mark.parametrize("fmt", ["e2m1", "i8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad, shift, qpad", [(0, 0, 0), (3, 1, 16), (8, 8, 0)])
+def test_quantize(rows, cols, fmt, dtype, pad, shift, qpad):
+    rng = np.random.default_rng([rows, cols, pad])
+    x = matrix(rng, rows, cols, dtype)
+    X = Dense(rows, cols, dtype, x, pad, shift)
+    n, t = Codes(fmt, rows, cols, qpad), Codes(fmt, cols, rows, qpad)
+    costa.costa_mx_quantize(X.c, "N", n.c, stream())
+    costa.costa_mx_quantize(X.c, "T", t.c, stream())
+    n.check(x)
+    t.check(x.T)
+    n2, t2 = Codes(fmt, rows, cols, qpad), Codes(fmt, cols, rows, qpad)
+    costa.costa_mx_quantize_both(X.c, n2.c, t2.c, stream())
+    n2.check(x)
+    t2.check(x.T)
+    Y = Dense(rows, cols, dtype, None, pad, shift)
+    costa.costa_mx_dequantize(n.c, Y.c, stream())
+    assert np.array_equal(Y.numpy(), _mx.rounded(fmt, x))
+
+
+@pytest.mark.parametrize("fmt", ["e2m1", "i8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_special_values(fmt, dtype):
+    """Ties, the largest and the smallest numbers, signed zeros, and blocks with infinities and NaN."""
+    tiny, big = 2.0 ** -126, 2.0 ** 127 * (2 - 2.0 ** -7)
+    rows = [np.arange(32) * 0.25, np.arange(32) / 64 + 1.0 / 128, -np.arange(32) * 0.125, np.full(32, big),
+            np.full(32, -tiny), np.arange(32) * tiny / 128, np.arange(32) * tiny * 0.75, np.zeros(32), -np.zeros(32),
+            np.where(np.arange(32) == 7, np.nan, 1.0), np.where(np.arange(32) == 31, np.inf, 1.0),
+            np.where(np.arange(32) == 0, -np.inf, 0.0), np.where(np.arange(32) % 2, big, tiny),
+            np.exp2(np.arange(32) - 140.0), np.exp2(-np.arange(32.0)) * 1.99, np.full(32, 2.0 ** -133)]
+    x = np.array(rows, np.float32)
+    x = _mx.bf16(x) if dtype == "bf16" else x
+    x = np.concatenate([x, np.roll(x, 5, 0)], 1)
+    X = Dense(*x.shape, dtype, x)
+    n, t = Codes(fmt, *x.shape), Codes(fmt, *x.T.shape)
+    costa.costa_mx_quantize_both(X.c, n.c, t.c, stream())
+    n.check(x)
+    t.check(x.T)
+    Y = Dense(*x.shape, dtype)
+    costa.costa_mx_dequantize(n.c, Y.c, stream())
+    assert np.array_equal(Y.numpy(), _mx.rounded(fmt, x), equal_nan=True)
+
+
+PRODUCTS = [(1, 1, 1), (1, 128, 32), (1, 300, 64), (2, 7, 33), (3, 130, 96), (8, 64, 128), (13, 501, 2200), (17, 129, 160),
+            (64, 64, 64), (127, 255, 257), (128, 128, 1024), (129, 257, 4096), (200, 1000, 777), (300, 520, 8200),
+            (1000, 33, 513), (5, 4096, 31), (16, 256, 16384)]
+
+
+@pytest.mark.parametrize("m, n, k", PRODUCTS)
+@pytest.mark.parametrize("dtype, alpha, beta, pad, qpad", [("f32", 1.0, 0.0, 0, 0), ("bf16", 1.0, 0.0, 0, 0),
+                                                           ("f32", -0.75, 0.3, 3, 16), ("bf16", 2.0, 1.0, 1, 48)])
+def test_product(m, n, k, dtype, alpha, beta, pad, qpad):
+    rng = np.random.default_rng([m, n, k])
+    A, a = codes_of("e2m1", matrix(rng, m, k, "f32"), qpad)
+    B, b = codes_of("e2m1", matrix(rng, n, k, "f32", 0.02), qpad)
+    c = matrix(rng, m, n, dtype)
+    C = Dense(m, n, dtype, c if beta else np.full((m, n), np.nan), pad, pad)
+    costa.costa_mx_product(A.c, B.c, C.c, alpha, beta, stream())
+    check_product(C, a, b, c, np.float64(np.float32(alpha)), np.float64(np.float32(beta)), dtype, k)
+
+
+def check_product(C, a, b, c, alpha, beta, dtype, terms):
+    """The products are exact; each of `terms` additions in 32 bits, truncating or rounding, is off by 2^-23 of what
+    the sum of magnitudes bounds; then alpha, beta and the output's rounding."""
+    want = alpha * (a @ b.T) + (beta * c if beta else 0.0)
+    mag = np.abs(alpha) * (np.abs(a) @ np.abs(b).T)
+    tol = mag * (terms + 2) * 2.0 ** -23 + (3 * 2.0 ** -24 * np.abs(beta * c) if beta else 0.0) + 1e-38
+    close(C.numpy(), want, tol + 2 * EPS[dtype] * (np.abs(want) + tol))
+
+
+def test_product_without_columns():
+    A, B = Codes("e2m1", 3, 0), Codes("e2m1", 5, 0)
+    c = np.arange(15, dtype=np.float32).reshape(3, 5)
+    C = Dense(3, 5, "f32", c)
+    costa.costa_mx_product(A.c, B.c, C.c, 1.0, 0.5, stream())
+    assert np.array_equal(C.numpy(), c * 0.5)
+    costa.costa_mx_product(A.c, B.c, C.c, 1.0, 0.0, stream())
+    assert not C.numpy().any()
+
+
+def test_product_nan_stays_in_its_rows():
+    """A block of NaN reaches its own row of C and no other; so does one in B for columns."""
+    rng = np.random.default_rng(3)
+    x, w = matrix(rng, 70, 300, "f32"), matrix(rng, 90, 300, "f32")
+    x[:, :8], w[:, :8] = 1.0, 1.0
+    x[4, 70], w[11, 299], w[80, 0] = np.nan, np.inf, -np.inf
+    (A, a), (B, b) = codes_of("e2m1", x), codes_of("e2m1", w)
+    C = Dense(70, 90, "f32")
+    costa.costa_mx_product(A.c, B.c, C.c, stream=stream())
+    got = C.numpy()
+    nan = np.zeros((70, 90), bool)
+    nan[4], nan[:, 11], nan[:, 80] = True, True, True
+    assert np.array_equal(np.isnan(got), nan)
+    close(np.where(nan, 0, got), np.where(nan, 0, np.nan_to_num(a) @ np.nan_to_num(b).T),
+          302 * 2.0 ** -23 * (np.abs(np.nan_to_num(a)) @ np.abs(np.nan_to_num(b)).T) + 1e-38)
+
+
+def test_product_small_and_large_scales():
+    """Scales at both ends of their range, where the products still fit 32 bits."""
+    rng = np.random.default_rng(5)
+    a_codes, b_codes = rng.integers(0, 16, (40, 256), np.uint8), rng.integers(0, 16, (50, 256), np.uint8)
+    sa = rng.integers(60, 100, (40, 8)).astype(np.uint8)
+    sb = rng.integers(60, 100, (50, 8)).astype(np.uint8)
+    sa[3], sb[7] = 0, 250  # 2^-127 and 2^123: their product is in range
+    A = Codes("e2m1", 40, 256, packed=_mx.pack("e2m1", a_codes, sa, 256))
+    B = Codes("e2m1", 50, 256, packed=_mx.pack("e2m1", b_codes, sb, 256))
+    a, b = _mx.values("e2m1", a_codes, sa, 256), _mx.values("e2m1", b_codes, sb, 256)
+    C = Dense(40, 50, "f32")
+    costa.costa_mx_product(A.c, B.c, C.c, stream=stream())
+    close(C.numpy(), a @ b.T, 258 * 2.0 ** -23 * (np.abs(a) @ np.abs(b).T) + 2.0 ** -126)
+
+
+ACT_SHAPES = [(1, 1), (1, 4096), (3, 33), (16, 257), (70, 1000), (33, 64)]
+
+
+@pytest.mark.parametrize("rows, cols", ACT_SHAPES)
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gated, pad", [(False, 0), (True, 0), (True, 3), (False, 1)])
+def test_act(rows, cols, name, dtype, gated, pad):
+    rng = np.random.default_rng([rows, cols, pad])
+    x, g, dy = (matrix(rng, rows, cols, dtype) for _ in range(3))
+    X, Y, dY, dX = (Dense(rows, cols, dtype, v, pad, pad) for v in (x, None, dy, None))
+    G, dG = (Dense(rows, cols, dtype, g, pad, pad), Dense(rows, cols, dtype, None, pad, pad)) if gated else (None, None)
+    qx, qg = Codes("i8", rows, cols, 16), Codes("i8", rows, cols) if gated else None
+    c = lambda v: v.c if v is not None else None
+    costa.costa_mx_act_forward(name, X.c, c(G), Y.c, qx.c, c(qg), stream())
+    qx.check(x)
+    if gated:
+        qg.check(g)
+    costa.costa_mx_act_backward(name, qx.c, c(qg), dY.c, dX.c, c(dG), stream())
+    # the functions within 8 units of 32 bits of their largest term; the slope's terms are at most 1 + |x|
+    unit = 16 * 2.0 ** -24
+    x, g, dy = (v.astype(np.float64) for v in (x, g, dy))
+    one = np.abs(g) if gated else 1.0
+    y = _mx.act(name, x)[0] * (g if gated else 1.0)
+    close(Y.numpy(), y, unit * np.abs(x) * one + 2 * EPS[dtype] * np.abs(y) + 1e-38)
+    xr, gr = _mx.rounded("i8", x), _mx.rounded("i8", g) if gated else 1.0
+    back, slope = _mx.act(name, xr)
+    dx = dy * gr * slope
+    close(dX.numpy(), dx, np.abs(dy * gr) * unit * (1 + np.abs(xr)) + 2 * EPS[dtype] * np.abs(dx) + 1e-38)
+    if gated:
+        close(dG.numpy(), dy * back, np.abs(dy) * unit * np.abs(xr) + 2 * EPS[dtype] * np.abs(dy * back) + 1e-38)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_act_gradient_against_differences(name):
+    """Central differences of the forward pass at the checkpoint's values, in 64 bits on the definition's side and
+    through the kernel: the slope is that of the function that the forward pass computes."""
+    x = np.linspace(-6, 6, 96, dtype=np.float32).reshape(3, 32)
+    qx, xr = codes_of("i8", x)
+    one = Dense(3, 32, "f32", np.ones((3, 32)))
+    dX = Dense(3, 32, "f32")
+    costa.costa_mx_act_backward(name, qx.c, None, one.c, dX.c, None, stream())
+    h = 2.0 ** -6
+    ends = []
+    for d in (-h, h):
+        X, Y, q = Dense(3, 32, "f32", (xr + d).astype(np.float32)), Dense(3, 32, "f32"), Codes("i8", 3, 32)
+        costa.costa_mx_act_forward(name, X.c, None, Y.c, q.c, None, stream())
+        ends.append(Y.numpy())
+    slope = (ends[1] - ends[0]) / (2 * h)
+    # third derivatives are below 2: h^2 / 3; each Y off by at most 16 units of 32 bits of 6
+    close(dX.numpy(), slope, np.full((3, 32), h * h / 3 + 6 * 16 * 2.0 ** -24 / h + 1e-5))
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
+def test_act_nan(name):
+    x = np.zeros((2, 64), np.float32)
+    x[0, 3] = np.nan
+    X, Y, q = Dense(2, 64, "f32", x), Dense(2, 64, "f32"), Codes("i8", 2, 64)
+    costa.costa_mx_act_forward(name, X.c, None, Y.c, q.c, None, stream())
+    q.check(x)
+    assert np.array_equal(np.isnan(Y.numpy()), np.isnan(x))
+    dY, dX = Dense(2, 64, "f32", np.ones((2, 64))), Dense(2, 64, "f32")
+    costa.costa_mx_act_backward(name, q.c, None, dY.c, dX.c, None, stream())
+    want = np.zeros((2, 64), bool)
+    want[0, :32] = True
+    assert np.array_equal(np.isnan(dX.numpy()), want)
+
+
+GRADS = [(1, 1, 1), (1, 128, 64), (3, 5, 33), (17, 129, 96), (31, 64, 257), (64, 64, 64), (65, 300, 100), (128, 256, 256),
+         (200, 130, 520), (777, 100, 153), (4100, 72, 40), (33, 1000, 24), (5000, 8, 300)]
+
+
+@pytest.mark.parametrize("m, n, k", GRADS)
+@pytest.mark.parametrize("ytype, wtype, alpha, beta, pad, qpad", [
+    ("bf16", "f32", 1.0, 0.0, 0, 0), ("f32", "f32", 1.0, 0.0, 0, 0), ("bf16", "bf16", 0.5, 1.0, 3, 16),
+    ("f32", "bf16", 1.0, 0.0, 1, 0), ("bf16", "f32", -1.5, 0.3, 8, 32), ("f32", "f32", 1.0, 1.0, 4, 0)])
+def test_weight_grad(m, n, k, ytype, wtype, alpha, beta, pad, qpad):
+    rng = np.random.default_rng([m, n, k])
+    dy = matrix(rng, m, n, ytype, 1e-3)
+    dY = Dense(m, n, ytype, dy, pad, pad)
+    q, x = codes_of("i8", matrix(rng, m, k, "f32"), qpad)
+    w = matrix(rng, n, k, wtype)
+    dW = Dense(n, k, wtype, w if beta else np.full((n, k), np.nan), pad, 0)
+    costa.costa_mx_weight_grad(dY.c, q.c, dW.c, alpha, beta, stream())
+    # f32 gradients may be summed in three parts
+    check_product(dW, dy.T.astype(np.float64), x.T, w, np.float64(np.float32(alpha)), np.float64(np.float32(beta)), wtype,
+                  3 * m)
+
+
+def test_weight_grad_without_tokens():
+    w = np.arange(12, dtype=np.float32).reshape(3, 4)
+    dW, q = Dense(3, 4, "f32", w), Codes("i8", 0, 4)
+    costa.costa_mx_weight_grad(costa.costa_mx_dense("bf16", 0, 3, 0, 3), q.c, dW.c, 1.0, 2.0, stream())
+    assert np.array_equal(dW.numpy(), w * 2)
+    costa.costa_mx_weight_grad(costa.costa_mx_dense("bf16", 0, 3, 0, 3), q.c, dW.c, 1.0, 0.0, stream())
+    assert not dW.numpy().any()
+
+
+@pytest.mark.parametrize("ytype", ["f32", "bf16"])
+def test_weight_grad_small_and_large(ytype):
+    """Scales at both ends, where the checkpoint's values are subnormal or near the largest, and gradients to match."""
+    rng = np.random.default_rng(9)
+    m, n, k = 96, 40, 96
+    codes = rng.integers(-127, 128, (m, k)).astype(np.int8)
+    s = rng.integers(120, 134, (m, 3)).astype(np.uint8)
+    s[:, 0], s[:, 2] = rng.integers(0, 8, m), rng.integers(240, 254, m)
+    x = _mx.values("i8", codes, s, k)
+    q = Codes("i8", m, k, packed=_mx.pack("i8", codes, s, k, fill=GUARD))
+    for scale, cols in ((2.0 ** 60, slice(0, 32)), (1.0, slice(32, 64)), (2.0 ** -60, slice(64, 96))):
+        dy = matrix(rng, m, n, ytype, scale)
+        dW = Dense(n, k, "f32")
+        costa.costa_mx_weight_grad(Dense(m, n, ytype, dy).c, q.c, dW.c, stream=stream())
+        got, d = dW.numpy()[:, cols], dy.T.astype(np.float64)
+        mag = np.abs(d) @ np.abs(x[:, cols])
+        close(got, d @ x[:, cols], 3 * (m + 2) * 2.0 ** -23 * mag + 1e-38)
+
+
+def test_weight_grad_nan_stays_in_its_columns():
+    rng = np.random.default_rng(4)
+    x = matrix(rng, 50, 100, "f32")
+    x[7, 40] = np.nan
+    dy = np.ones((50, 20), np.float32)
+    dy[:, 3] = 0
+    dy[2, 5] = np.inf
+    q, xr = codes_of("i8", x)
+    dW = Dense(20, 100, "f32")
+    costa.costa_mx_weight_grad(Dense(50, 20, "f32", dy).c, q.c, dW.c, stream=stream())
+    got = dW.numpy()
+    with np.errstate(invalid="ignore"):
+        want = np.einsum("tn,tk->nk", dy.astype(np.float64), xr)
+    assert np.isnan(got[:, 32:64]).all()
+    rest = np.r_[0:32, 64:100]
+    others = np.r_[0:5, 6:20]
+    assert np.isfinite(got[np.ix_(others, rest)]).all()
+    assert not np.isfinite(got[5, rest]).any()
+    close(got[np.ix_(others, rest)], want[np.ix_(others, rest)],
+          (150 * 2.0 ** -23 * (np.abs(dy.T) @ np.abs(np.nan_to_num(xr))))[np.ix_(others, rest)] + 1e-38)
+
+
+def test_weight_grad_against_differences():
+    """<dW, V> is the derivative of sum(dY * (X W^T)) along V: differences of that (linear) function in 64 bits."""
+    rng = np.random.default_rng(6)
+    m, n, k = 60, 30, 50
+    dy, w, v = rng.standard_normal((m, n)).astype(np.float32), rng.standard_normal((n, k)), rng.standard_normal((n, k))
+    q, x = codes_of("i8", matrix(rng, m, k, "f32"))
+    dW = Dense(n, k, "f32")
+    costa.costa_mx_weight_grad(Dense(m, n, "f32", dy).c, q.c, dW.c, stream=stream())
+    f = lambda u: float(np.sum(dy.astype(np.float64) * (x @ u.T)))
+    diff = (f(w + v) - f(w - v)) / 2
+    mag = float(np.sum((np.abs(dy).T.astype(np.float64) @ np.abs(x)) * np.abs(v)))
+    assert abs(float(np.sum(dW.numpy() * v)) - diff) <= mag * 3 * (m + 2) * 2.0 ** -23
+
+
+def test_repeated_calls_give_the_same_bits():
+    rng = np.random.default_rng(8)
+    A, _ = codes_of("e2m1", matrix(rng, 9, 5000, "f32"))
+    B, _ = codes_of("e2m1", matrix(rng, 700, 5000, "f32"))
+    q, _ = codes_of("i8", matrix(rng, 3000, 90, "f32"))
+    dY = Dense(3000, 70, "f32", matrix(rng, 3000, 70, "f32"))
+    seen = []
+    for _ in range(3):
+        C, dW = Dense(9, 700, "f32"), Dense(70, 90, "f32")
+        costa.costa_mx_product(A.c, B.c, C.c, stream=stream())
+        costa.costa_mx_weight_grad(dY.c, q.c, dW.c, stream=stream())
+        seen.append((C.numpy(), dW.numpy()))
+    for c, w in seen[1:]:
+        assert np.array_equal(c, seen[0][0]) and np.array_equal(w, seen[0][1])
+
+
+def test_streams_and_graph():
+    """A layer's step on a side stream, then captured in a graph and replayed on other inputs."""
+    rng = np.random.default_rng(11)
+    m, n, k = 40, 200, 160
+    side = torch.cuda.Stream()
+    X, w = Dense(m, k, "bf16", matrix(rng, m, k, "bf16")), matrix(rng, n, k, "f32")
+    B, b = codes_of("e2m1", w)
+    qx, q8, C, dW = Codes("e2m1", m, k), Codes("i8", m, k), Dense(m, n, "f32"), Dense(n, k, "f32")
+    dy = matrix(rng, m, n, "bf16")
+    dY = Dense(m, n, "bf16", dy)
+
+    def step():
+        s = stream()
+        costa.costa_mx_quantize(X.c, "N", qx.c, s)
+        costa.costa_mx_quantize(X.c, "N", q8.c, s)
+        costa.costa_mx_product(qx.c, B.c, C.c, stream=s)
+        costa.costa_mx_weight_grad(dY.c, q8.c, dW.c, stream=s)
+
+    def check(x):
+        check_product(C, _mx.rounded("e2m1", x), b, None, 1.0, 0.0, "f32", k)
+        check_product(dW, dy.T.astype(np.float64), _mx.rounded("i8", x).T, None, 1.0, 0.0, "f32", 3 * m)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    check(X.numpy())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(2):
+        X.view.copy_(torch.from_numpy(matrix(rng, m, k, "bf16")))
+        graph.replay()
+        torch.cuda.synchronize()
+        check(X.view.double().cpu().numpy())
+
+
+def test_storage_refusals():
+    """Host memory and matrices that leave their allocation are refused before any kernel runs."""
+    host = np.zeros(4096, np.uint8)
+    x = torch.zeros(64, 64, device="cuda")
+    q = Codes("e2m1", 64, 64)
+    n = costa.costa_kernel_launch_count()
+    at = -(-host.ctypes.data // 16) * 16
+    for bad in (costa.costa_mx_dense("f32", 4, 64, at, 64),
+                costa.costa_mx_dense("f32", 4, 64, x.data_ptr(), 1 << 33)):
+        with pytest.raises(costa.CostaError) as e:
+            costa.costa_mx_quantize(bad, "N", costa.costa_mx_matrix("e2m1", 4, 64, q.codes.data_ptr(),
+                                                                    q.scales.data_ptr(), 32), stream())
+        assert costa.STATUS_NAMES[e.value.status] == "LAYOUT"
+    with pytest.raises(costa.CostaError) as e:
+        costa.costa_mx_quantize(costa.costa_mx_dense("f32", 64, 64, x.data_ptr(), 64), "N",
+                                costa.costa_mx_matrix("e2m1", 64, 64, q.codes.data_ptr(), at, 32), stream())
+    assert costa.STATUS_NAMES[e.value.status] == "LAYOUT"
+    assert costa.costa_kernel_launch_count() == n
+
+
+def test_offsets_beyond_32_bits():
+    """Matrices of more than 2^32 elements: codes beyond 2 GB, dense rows beyond 8 GB."""
+    rows, cols = 70000, 65536
+    least, nc, ns = _mx.sizes("e2m1", rows, cols)
+    x = torch.randn(rows, 256, device="cuda", dtype=torch.bfloat16).repeat(1, cols // 256)
+    codes = torch.empty(nc, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(ns, dtype=torch.uint8, device="cuda")
+    Q = costa.costa_mx_matrix("e2m1", rows, cols, codes.data_ptr(), scales.data_ptr(), least)
+    costa.costa_mx_quantize(costa.costa_mx_dense("bf16", rows, cols, x.data_ptr(), cols), "N", Q, stream())
+    at = [0, 1, 127, 33333, 65535, 65536, 69999]
+    picked = x[at].double().cpu().numpy()
+    want = _mx.rounded("e2m1", picked)
+    got = codes.view(rows, least)[at].cpu().numpy()
+    assert np.array_equal(got, _mx.pack("e2m1", *_mx.quantize("e2m1", picked), cols)[0])
+    token, t = codes_of("e2m1", matrix(np.random.default_rng(2), 2, cols, "f32"))
+    C = Dense(2, rows, "f32")
+    costa.costa_mx_product(token.c, Q, C.c, stream=stream())
+    close(C.numpy()[:, at], t @ want.T, (cols + 2) * 2.0 ** -23 * (np.abs(t) @ np.abs(want).T))
+    del x
+    y = torch.empty(rows, cols, device="cuda", dtype=torch.bfloat16)
+    costa.costa_mx_dequantize(Q, costa.costa_mx_dense("bf16", rows, cols, y.data_ptr(), cols), stream())
+    assert np.array_equal(y[at].double().cpu().numpy(), want)
