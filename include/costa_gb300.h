@@ -754,6 +754,13 @@ costa_status costa_mx_act_backward(costa_mx_act act, const costa_mx_matrix *QX, 
 costa_status costa_mx_weight_grad(const costa_mx_dense *dY, const costa_mx_matrix *QX, float alpha,
                                   float beta, const costa_mx_dense *dW, void *stream);
 
+/* Diagnostics: the thread blocks of costa_mx_product and costa_mx_weight_grad
+ * that gave up a wait on the current device since the library was loaded.
+ * Their waits for copies and tensor cores are bounded; a block that gives one
+ * up leaves its part of the output undefined.  0 unless the device misbehaves.
+ * Synchronizes the device.  Errors: INVALID_ARG, CUDA. */
+costa_status costa_mx_failures(int64_t *count);
+
 /* ABI version of this header (1). */
 int costa_abi_version(void);
 

@@ -115,6 +115,7 @@ def _load():
         "costa_mx_act_forward": [I, P, P, P, P, P, P],
         "costa_mx_act_backward": [I, P, P, P, P, P, P],
         "costa_mx_weight_grad": [P, P, F, F, P, P],
+        "costa_mx_failures": [P],
     }
     for name, args in sigs.items():
         f = getattr(lib, name)
@@ -777,3 +778,10 @@ def costa_mx_weight_grad(dY: bytes, QX: bytes, dW: bytes, alpha: float = 1.0, be
                          stream: int = 0) -> None:
     """dW = alpha * dY^T X + beta * dW with X from its "i8" checkpoint QX."""
     _check(_lib.costa_mx_weight_grad(dY, QX, alpha, beta, dW, stream))
+
+
+def costa_mx_failures() -> int:
+    """Thread blocks of the products that gave up a wait (0 on a sound device)."""
+    n = ctypes.c_int64()
+    _check(_lib.costa_mx_failures(ctypes.byref(n)))
+    return n.value

@@ -8,6 +8,7 @@
 
 #include "costa_internal.h"
 #include "mx.h"
+#include "mx_host.h"
 
 namespace {
 
@@ -292,6 +293,16 @@ costa_status costa_mx_weight_grad(const costa_mx_dense *dY, const costa_mx_matri
     COSTA_MX_CHECK(Access().dense(dY, "dY").codes(QX, "QX").dense(dW, "dW").st);
     return done(launch_mx_weight_grad(*dY, *QX, alpha, beta, *dW, static_cast<cudaStream_t>(stream)),
                 "costa_mx_weight_grad");
+}
+
+costa_status costa_mx_failures(int64_t *count) {
+    if (!count) return bad(COSTA_ERR_INVALID_ARG, "count is null");
+    unsigned a = 0, b = 0;
+    cudaError_t e = mx_product_failures(&a);
+    if (e == cudaSuccess) e = mx_grad_failures(&b);
+    if (e != cudaSuccess) return done(e, "costa_mx_failures");
+    *count = int64_t(a) + b;
+    return COSTA_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,60 @@
+// Host helpers of the low-bit products, and C = beta C.
+#include "costa_internal.h"
+#include "mx_device.cuh"
+#include "mx_host.h"
+
+namespace costa {
+namespace {
+
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                              const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+    static const EncodeFn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeFn>(f);
+    }();
+    return fn;
+}
+
+template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t rows, int64_t cols, float beta) {
+    for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
+        for (int64_t j = threadIdx.x; j < cols; j += blockDim.x) {
+            T *at = c + i * ld + j;
+            *at = mx::from_float<T>(beta == 0.0f ? 0.0f : beta * mx::to_float(*at));
+        }
+}
+
+}  // namespace
+
+cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint64_t rows, uint64_t pitch,
+                        uint32_t box_rows) {
+    const EncodeFn encode = encode_fn();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {width, rows}, strides[1] = {pitch};
+    const cuuint32_t box[2] = {128, box_rows}, step[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s) {
+    const unsigned grid = static_cast<unsigned>(C.rows < 65536 ? C.rows : 65536);
+    if (C.type == COSTA_MX_F32)
+        scale_kernel<<<grid, 256, 0, s>>>(static_cast<float *>(C.ptr), C.ld, C.rows, C.cols, beta);
+    else
+        scale_kernel<<<grid, 256, 0, s>>>(static_cast<__nv_bfloat16 *>(C.ptr), C.ld, C.rows, C.cols, beta);
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+}  // namespace costa

@@ -1,48 +1,293 @@
-// C = alpha A B^T + beta C with A and B in E2M1.
+// C = alpha A B^T + beta C with A (m x k) and B (n x k) in E2M1, on the tensor
+// cores' block-scaled 4-bit products.
+//
+// One thread block takes a tile of 128 rows of B (the lanes of tensor memory)
+// and NT rows of A (its columns), so that a warp's lanes hold neighbouring
+// elements of a row of C and few rows of A need few columns.  Warp 4 brings
+// operands and scales into a ring of stages of 256 columns of k, one thread of
+// warp 5 issues the products, warps 0 to 3 write the tile out.
+#include <algorithm>
+
 #include "costa_internal.h"
-#include "mx_device.cuh"
+#include "mx_tc.cuh"
 
 namespace costa {
 namespace mx {
 namespace {
 
-constexpr int kTile = 32;
+constexpr int kThreads = 192;
+constexpr int kRows = 128;   // rows of B in a tile
+constexpr int kStageK = 256; // elements of k in a stage: 128 bytes of a row, 2 tiles of scales
+
+__device__ unsigned g_failed;
+
+struct Params {
+    const uint8_t *a_scales, *b_scales;
+    void *c;
+    int64_t ldc;
+    int64_t m, n;
+    int steps;           // products of 64 elements over k
+    int scale_tiles;     // tiles of scales over k
+    int n_tiles, m_tiles;
+    float alpha, beta;
+};
+
+// The columns of tensor memory and the stages of a tile of NT rows of A.
+template <int NT> struct Shape {
+    static constexpr int bands = NT > 128 ? 2 : 1;  // of 128 rows of A's scales
+    // Two sums of NT columns, so that one is written out while the next
+    // builds.  Two of 256 would leave no room for the scales: they share
+    // columns 208 .. 255, which the epilogue reads first (or, of the second
+    // sum, also first) and then hands over.
+    static constexpr int second = NT == 256 ? 208 : NT;
+    static constexpr int scales = NT == 256 ? 464 : 2 * NT;
+    static constexpr int scale_cols = 8 + 8 * bands;  // of a stage: 2 tiles of B, 2 of each band of A
+    static constexpr int used = scales + 2 * scale_cols;
+    static constexpr int cols = used <= 64 ? 64 : used <= 128 ? 128 : used <= 256 ? 256 : 512;
+    static constexpr int b_bytes = kRows * 128, a_bytes = NT * 128, sf_bytes = 1024 * (1 + bands);
+    static constexpr int stage = (b_bytes + a_bytes + sf_bytes + 1023) / 1024 * 1024;
+    static constexpr int stages = NT == 256 ? 4 : NT == 128 ? 5 : 4;
+    static constexpr int smem = stages * stage + 1024;
+    static_assert(kRows * NT * 4 <= stages * stage, "a tile's partial sums fit the stages");
+};
+
+template <int NT, typename T>
+__global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ CUtensorMap a_map,
+                                                           const __grid_constant__ CUtensorMap b_map, const Params p,
+                                                           const int split) {
+    using S = Shape<NT>;
+    constexpr int kLag = NT == 256 ? 1 : 2;  // the tile whose epilogue a tile waits for
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::stages + 4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t failed_word;
+    volatile uint32_t *failed = &failed_word;
+    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t bar0 = smem_addr(bars);
+    auto full = [&](int s) { return bar0 + 8 * s; };
+    auto empty = [&](int s) { return bar0 + 8 * (S::stages + s); };
+    auto sum_full = [&](int i) { return bar0 + 8 * (2 * S::stages + i); };
+    auto sum_empty = [&](int i) { return bar0 + 8 * (2 * S::stages + 2 + i); };
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    if (threadIdx.x == 0) {
+        failed_word = 0;
+        for (int s = 0; s < S::stages; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(sum_full(i), 1);
+            bar_init(sum_empty(i), 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) tmem_alloc(&tmem_slot, S::cols);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    // This block's share of k, in stages; and its tiles.
+    const int stages_k = (p.steps + 3) / 4;
+    const int part = split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int k_first = static_cast<int>(int64_t(stages_k) * part / split);
+    const int k_last = static_cast<int>(int64_t(stages_k) * (part + 1) / split);
+    const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / split, stride = gridDim.x / split;
+
+    if (warp == 4) {
+        if (elect_one()) {
+            int it = 0;
+            for (int t = first; t < tiles; t += stride) {
+                const int nt = t / p.m_tiles, mt = t % p.m_tiles;
+                for (int k = k_first; k < k_last; ++k, ++it) {
+                    const int s = it % S::stages;
+                    if (it >= S::stages && !bar_wait(empty(s), (it / S::stages - 1) & 1, failed)) break;
+                    const uint32_t at = ring + s * S::stage, sf = at + S::b_bytes + S::a_bytes;
+                    const int sft = min(2, p.scale_tiles - 2 * k);  // tiles of scales of this stage
+                    // bands of A's scales that exist
+                    const int bands = S::bands == 2 && int64_t(mt) * NT + 128 < p.m ? 2 : 1;
+                    bar_expect(full(s), S::b_bytes + S::a_bytes + (1 + bands) * sft * 512);
+                    tma_load_2d(at, &b_map, k * 128, nt * kRows, full(s));
+                    tma_load_2d(at + S::b_bytes, &a_map, k * 128, mt * NT, full(s));
+                    bulk_load(sf, p.b_scales + (int64_t(nt) * p.scale_tiles + 2 * k) * 512, sft * 512, full(s));
+                    const int64_t band = int64_t(mt) * NT / 128;
+                    for (int b = 0; b < bands; ++b)
+                        bulk_load(sf + 1024 * (1 + b), p.a_scales + ((band + b) * p.scale_tiles + 2 * k) * 512, sft * 512,
+                                  full(s));
+                }
+                if (*failed) break;
+            }
+            // Failed: copies in flight still write this block's memory.
+            if (*failed)
+                for (int s = 0; s < S::stages && s < it; ++s) {
+                    const uint32_t parity = ((it - 1 - s) / S::stages) & 1;
+                    const long long start = clock64();
+                    while (!bar_try(full(s), parity) && clock64() - start < kWaitClocks) {}
+                }
+        }
+    } else if (warp == 5) {
+        if (elect_one()) {
+            int it = 0, done = 0;
+            for (int t = first; t < tiles && !*failed; t += stride, ++done) {
+                const uint32_t d = tmem + (done & 1 ? S::second : 0);
+                const int before = done - kLag;
+                if (before >= 0 && !bar_wait(sum_empty(before & 1), (before >> 1) & 1, failed)) break;
+                fence_after();
+                for (int k = k_first; k < k_last; ++k, ++it) {
+                    const int s = it % S::stages;
+                    if (!bar_wait(full(s), (it / S::stages) & 1, failed)) break;
+                    fence_after();
+                    const uint32_t at = ring + s * S::stage, sf = at + S::b_bytes + S::a_bytes;
+                    const uint32_t sfd = tmem + S::scales + (it & 1) * S::scale_cols;
+                    const int steps = min(4, p.steps - 4 * k);
+                    // columns of the scales: B's two tiles, then A's as (k tile, band)
+                    for (int c = 0; 2 * c < steps; ++c) {
+                        scales_to_tmem(sfd + 4 * c, scales_desc(sf + 512 * c));
+                        for (int b = 0; b < S::bands; ++b)
+                            scales_to_tmem(sfd + 8 + 4 * (S::bands * c + b), scales_desc(sf + 1024 * (1 + b) + 512 * c));
+                    }
+                    const uint64_t da = operand_desc(at, 16, 1024), db = operand_desc(at + S::b_bytes, 16, 1024);
+                    for (int q = 0; q < steps; ++q)
+                        mma_e2m1(d, da + 2 * q, db + 2 * q, idesc_e2m1(NT, (q & 1) * 2), sfd + 4 * (q >> 1),
+                                 sfd + 8 + 4 * S::bands * (q >> 1), k > k_first || q > 0);
+                    mma_commit(empty(s));
+                }
+                if (*failed) break;
+                mma_commit(sum_full(done & 1));
+            }
+        }
+    } else {
+        T *const c = static_cast<T *>(p.c);
+        int done = 0;
+        for (int t = first; t < tiles; t += stride, ++done) {
+            const int nt = t / p.m_tiles, mt = t % p.m_tiles;
+            if (!__all_sync(~0u, bar_wait(sum_full(done & 1), (done >> 1) & 1, failed))) break;
+            fence_after();
+            const uint32_t d = tmem + (done & 1 ? S::second : 0) + (uint32_t(warp * 32) << 16);
+            const int64_t row0 = int64_t(mt) * NT, col = int64_t(nt) * kRows + warp * 32 + lane;
+            constexpr int kChunks = NT / 16;
+            // the shared columns first: chunks 13 .. 15 of the first sum, 0 .. 2 of the second
+            const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0;
+            for (int j = 0; j < kChunks; ++j) {
+                const int ch = (j + shift) % kChunks;
+                const int64_t row = row0 + ch * 16;
+                if (row < p.m) {
+                    uint32_t r[16];
+                    tmem_ld16(d + ch * 16, r);
+                    tmem_wait_ld();
+                    if (split > 1) {
+                        float *part_sums = reinterpret_cast<float *>(raw + (ring - smem_addr(raw)));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            part_sums[(ch * 16 + i) * kRows + warp * 32 + lane] = __uint_as_float(r[i]);
+                    } else if (col < p.n) {
+                        T *at = c + row * p.ldc + col;
+                        const int rows = static_cast<int>(min(int64_t(16), p.m - row));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (i < rows) {
+                                float v = p.alpha * __uint_as_float(r[i]);
+                                if (p.beta != 0.0f) v += p.beta * to_float(at[i * p.ldc]);
+                                at[i * p.ldc] = from_float<T>(v);
+                            }
+                    }
+                }
+                if (kLag == 1 && j == 2) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(sum_empty(done & 1));
+                }
+            }
+            if (kLag != 1) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(sum_empty(done & 1));
+            }
+        }
+    }
+
+    if (split > 1) {  // one tile to a cluster: each block adds a share of its elements, in the order of k
+        __syncwarp();
+        cluster_sync();
+        const int64_t row0 = int64_t(first % p.m_tiles) * NT;
+        const int rows = static_cast<int>(min(int64_t(NT), p.m - row0)), n0 = first / p.m_tiles * kRows;
+        const int total = rows * kRows;
+        for (int e = part * kThreads + threadIdx.x; e < total; e += split * kThreads) {
+            float v = 0.0f;
+            for (int r = 0; r < split; ++r) v += cluster_load(ring + 4 * e, r);
+            const int64_t col = int64_t(n0) + e % kRows;
+            if (col < p.n) {
+                T *at = static_cast<T *>(p.c) + (row0 + e / kRows) * p.ldc + col;
+                v *= p.alpha;
+                if (p.beta != 0.0f) v += p.beta * to_float(*at);
+                *at = from_float<T>(v);
+            }
+        }
+        cluster_sync();  // no block leaves while others read its sums
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 5) {
+        fence_after();
+        tmem_free(tmem, S::cols);
+    }
+    if (threadIdx.x == 0 && *failed) atomicAdd(&g_failed, 1u);
+}
+
+template <int NT, typename T>
+cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alpha, float beta, const costa_mx_dense &C,
+                   int sms, cudaStream_t s) {
+    using S = Shape<NT>;
+    const int64_t nb = mx_blocks(A.cols);
+    CUtensorMap a_map, b_map;
+    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, NT);
+    if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows);
+    if (e != cudaSuccess) return e;
+    Params p;
+    p.a_scales = static_cast<const uint8_t *>(A.scales);
+    p.b_scales = static_cast<const uint8_t *>(B.scales);
+    p.c = C.ptr;
+    p.ldc = C.ld;
+    p.m = C.rows;
+    p.n = C.cols;
+    p.steps = static_cast<int>(mx_ceil(nb, 2));
+    p.scale_tiles = static_cast<int>(mx_scale_tiles(A.cols));
+    p.n_tiles = static_cast<int>(mx_ceil(C.cols, kRows));
+    p.m_tiles = static_cast<int>(mx_ceil(C.rows, NT));
+    p.alpha = alpha;
+    p.beta = beta;
+    const int64_t tiles = int64_t(p.n_tiles) * p.m_tiles;
+    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+    const int stages_k = (p.steps + 3) / 4;
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= 2 * sms && stages_k >= 4 * split) split *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(split > 1 ? tiles * split : std::min<int64_t>(tiles, sms)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {static_cast<unsigned>(split), 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaFuncSetAttribute(product_kernel<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
+    if (e != cudaSuccess) return e;
+    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, p, split);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
 
 template <typename T>
-__global__ void __launch_bounds__(256) product_kernel(costa_mx_matrix A, costa_mx_matrix B, float alpha, float beta,
-                                                      T *C, int64_t ldc, unsigned col_tiles) {
-    __shared__ float a[kTile][33], b[kTile][33];
-    const int64_t i0 = int64_t(blockIdx.x / col_tiles) * kTile, j0 = int64_t(blockIdx.x % col_tiles) * kTile;
-    const int64_t tiles = (((A.cols + 31) >> 5) + 3) >> 2;
-    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-    for (int64_t k = 0; k < A.cols; k += 32) {
-        {
-            const bool is_a = threadIdx.x < 128;
-            const int t = threadIdx.x & 127, r = t / 4, g = t % 4;
-            const costa_mx_matrix &M = is_a ? A : B;
-            const int64_t row = (is_a ? i0 : j0) + r;
-            float v[8] = {};
-            if (row < M.rows) {
-                const float unit = pow2(static_cast<const uint8_t *>(M.scales)[scale_at(row, k >> 5, tiles)]);
-                e2m1_to8(*reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(M.codes) + row * M.ld + k / 2 +
-                                                             4 * g),
-                         unit, v);
-            }
-            for (int i = 0; i < 8; ++i) (is_a ? a : b)[r][8 * g + i] = v[i];
-        }
-        __syncthreads();
-        for (int q = 0; q < 32; ++q)
-            for (int i = 0; i < 4; ++i) acc[i] += a[ty + 8 * i][q] * b[tx][q];
-        __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = i0 + ty + 8 * i, col = j0 + tx;
-        if (row < A.rows && col < B.rows) {
-            T *c = C + row * ldc + col;
-            *c = from_float<T>(beta == 0.0f ? alpha * acc[i] : alpha * acc[i] + beta * to_float(*c));
-        }
-    }
+cudaError_t by_rows(const costa_mx_matrix &A, const costa_mx_matrix &B, float alpha, float beta, const costa_mx_dense &C,
+                    int sms, cudaStream_t s) {
+    if (C.rows <= 16) return launch<16, T>(A, B, alpha, beta, C, sms, s);
+    if (C.rows <= 32) return launch<32, T>(A, B, alpha, beta, C, sms, s);
+    if (C.rows <= 64) return launch<64, T>(A, B, alpha, beta, C, sms, s);
+    if (C.rows <= 128 || mx_ceil(C.rows, 256) * mx_ceil(C.cols, kRows) < sms)
+        return launch<128, T>(A, B, alpha, beta, C, sms, s);
+    return launch<256, T>(A, B, alpha, beta, C, sms, s);
 }
 
 }  // namespace
@@ -50,15 +295,17 @@ __global__ void __launch_bounds__(256) product_kernel(costa_mx_matrix A, costa_m
 
 cudaError_t launch_mx_product(const costa_mx_matrix &A, const costa_mx_matrix &B, float alpha, float beta,
                               const costa_mx_dense &C, cudaStream_t s) {
-    const unsigned cols = static_cast<unsigned>(mx_ceil(C.cols, mx::kTile));
-    const unsigned grid = static_cast<unsigned>(cols * mx_ceil(C.rows, mx::kTile));
-    if (C.type == COSTA_MX_F32)
-        mx::product_kernel<<<grid, 256, 0, s>>>(A, B, alpha, beta, static_cast<float *>(C.ptr), C.ld, cols);
-    else
-        mx::product_kernel<<<grid, 256, 0, s>>>(A, B, alpha, beta, static_cast<__nv_bfloat16 *>(C.ptr), C.ld, cols);
-    const cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) count_launch();
-    return e;
+    if (A.cols == 0) return launch_mx_scale(beta, C, s);
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    return C.type == COSTA_MX_F32 ? mx::by_rows<float>(A, B, alpha, beta, C, sms, s)
+                                  : mx::by_rows<__nv_bfloat16>(A, B, alpha, beta, C, sms, s);
+}
+
+cudaError_t mx_product_failures(unsigned *count) {
+    return cudaMemcpyFromSymbol(count, mx::g_failed, sizeof *count);
 }
 
 }  // namespace costa
