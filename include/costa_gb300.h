@@ -749,7 +749,8 @@ costa_status costa_mx_act_backward(costa_mx_act act, const costa_mx_matrix *QX, 
  * from the checkpoint QX of X (m x k, I8): dY (m x n) f32 or bf16, dW (n x k)
  * f32 or bf16.  The products of dY's elements with the checkpoint's values are
  * exact, for f32 dY too (of magnitude 2^-109 or more; bits below 2^-133 are
- * dropped), and are summed in 32 bits.  With beta == 0 dW is not read; m == 0 gives beta * dW.  Errors: INVALID_ARG, SHAPE, DTYPE (a format
+ * dropped; an infinite element gives NaN where dY is f32), and are summed in
+ * 32 bits.  With beta == 0 dW is not read; m == 0 gives beta * dW.  Errors: INVALID_ARG, SHAPE, DTYPE (a format
  * other than I8), LAYOUT, CUDA. */
 costa_status costa_mx_weight_grad(const costa_mx_dense *dY, const costa_mx_matrix *QX, float alpha,
                                   float beta, const costa_mx_dense *dW, void *stream);

@@ -24,6 +24,19 @@ EncodeFn encode_fn() {
     return fn;
 }
 
+cudaError_t tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t width, uint64_t rows,
+                       uint64_t pitch, uint32_t box_width, uint32_t box_rows, bool swizzle) {
+    const EncodeFn encode = encode_fn();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {width, rows}, strides[1] = {pitch};
+    const cuuint32_t box[2] = {box_width, box_rows}, step[2] = {1, 1};
+    const CUresult r = encode(map, type, 2, const_cast<void *>(base), dims, strides, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t rows, int64_t cols, float beta) {
     for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
         for (int64_t j = threadIdx.x; j < cols; j += blockDim.x) {
@@ -35,15 +48,13 @@ template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t row
 }  // namespace
 
 cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint64_t rows, uint64_t pitch,
+                        uint32_t box_rows, bool swizzle) {
+    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, width, rows, pitch, 128, box_rows, swizzle);
+}
+
+cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t ld,
                         uint32_t box_rows) {
-    const EncodeFn encode = encode_fn();
-    if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {width, rows}, strides[1] = {pitch};
-    const cuuint32_t box[2] = {128, box_rows}, step[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, 2 * ld, 64, box_rows, true);
 }
 
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s) {

@@ -10,9 +10,12 @@
 
 namespace costa {
 
-// The 2-D tensor map of bytes (128-byte swizzle, zeros outside): `width` bytes
-// x `rows`, `pitch` bytes from row to row, boxes of 128 bytes x `box_rows`.
+// 2-D tensor maps, zeros outside, 128-byte swizzle: of bytes, `width` bytes x
+// `rows`, `pitch` bytes from row to row, in boxes of 128 bytes x `box_rows`
+// (swizzled or not); of bf16, in boxes of 64 elements.
 cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint64_t rows, uint64_t pitch,
+                        uint32_t box_rows, bool swizzle);
+cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t ld,
                         uint32_t box_rows);
 // C = beta C (0 without reading C for beta == 0): products over nothing.
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s);

@@ -17,19 +17,16 @@ namespace {
 
 constexpr int kThreads = 192;
 constexpr int kRows = 128;   // rows of B in a tile
-constexpr int kStageK = 256; // elements of k in a stage: 128 bytes of a row, 2 tiles of scales
+// A stage holds 256 elements of k: 128 bytes of a row, 2 tiles of scales.
 
 __device__ unsigned g_failed;
 
 struct Params {
     const uint8_t *a_scales, *b_scales;
-    void *c;
-    int64_t ldc;
-    int64_t m, n;
+    int64_t m;           // rows of A
     int steps;           // products of 64 elements over k
     int scale_tiles;     // tiles of scales over k
     int n_tiles, m_tiles;
-    float alpha, beta;
 };
 
 // The columns of tensor memory and the stages of a tile of NT rows of A.
@@ -52,9 +49,9 @@ template <int NT> struct Shape {
 };
 
 template <int NT, typename T>
-__global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ CUtensorMap a_map,
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap a_map,
                                                            const __grid_constant__ CUtensorMap b_map, const Params p,
-                                                           const int split) {
+                                                           const Output<T> out, const int split) {
     using S = Shape<NT>;
     constexpr int kLag = NT == 256 ? 1 : 2;  // the tile whose epilogue a tile waits for
     extern __shared__ uint8_t raw[];
@@ -63,6 +60,7 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     __shared__ uint32_t failed_word;
     volatile uint32_t *failed = &failed_word;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
+    float *const part_sums = reinterpret_cast<float *>(raw + (ring - smem_addr(raw)));
     const uint32_t bar0 = smem_addr(bars);
     auto full = [&](int s) { return bar0 + 8 * s; };
     auto empty = [&](int s) { return bar0 + 8 * (S::stages + s); };
@@ -118,13 +116,6 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
                 }
                 if (*failed) break;
             }
-            // Failed: copies in flight still write this block's memory.
-            if (*failed)
-                for (int s = 0; s < S::stages && s < it; ++s) {
-                    const uint32_t parity = ((it - 1 - s) / S::stages) & 1;
-                    const long long start = clock64();
-                    while (!bar_try(full(s), parity) && clock64() - start < kWaitClocks) {}
-                }
         }
     } else if (warp == 5) {
         if (elect_one()) {
@@ -158,74 +149,29 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
             }
         }
     } else {
-        T *const c = static_cast<T *>(p.c);
         int done = 0;
         for (int t = first; t < tiles; t += stride, ++done) {
-            const int nt = t / p.m_tiles, mt = t % p.m_tiles;
             if (!__all_sync(~0u, bar_wait(sum_full(done & 1), (done >> 1) & 1, failed))) break;
             fence_after();
-            const uint32_t d = tmem + (done & 1 ? S::second : 0) + (uint32_t(warp * 32) << 16);
-            const int64_t row0 = int64_t(mt) * NT, col = int64_t(nt) * kRows + warp * 32 + lane;
+            const uint32_t d = tmem + (done & 1 ? S::second : 0);
             constexpr int kChunks = NT / 16;
             // the shared columns first: chunks 13 .. 15 of the first sum, 0 .. 2 of the second
             const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0;
             for (int j = 0; j < kChunks; ++j) {
-                const int ch = (j + shift) % kChunks;
-                const int64_t row = row0 + ch * 16;
-                if (row < p.m) {
-                    uint32_t r[16];
-                    tmem_ld16(d + ch * 16, r);
-                    tmem_wait_ld();
-                    if (split > 1) {
-                        float *part_sums = reinterpret_cast<float *>(raw + (ring - smem_addr(raw)));
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            part_sums[(ch * 16 + i) * kRows + warp * 32 + lane] = __uint_as_float(r[i]);
-                    } else if (col < p.n) {
-                        T *at = c + row * p.ldc + col;
-                        const int rows = static_cast<int>(min(int64_t(16), p.m - row));
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (i < rows) {
-                                float v = p.alpha * __uint_as_float(r[i]);
-                                if (p.beta != 0.0f) v += p.beta * to_float(at[i * p.ldc]);
-                                at[i * p.ldc] = from_float<T>(v);
-                            }
-                    }
-                }
-                if (kLag == 1 && j == 2) {
+                tile_out16(out, d, (j + shift) % kChunks, int64_t(t % p.m_tiles) * NT, int64_t(t / p.m_tiles) * kRows,
+                           split > 1 ? part_sums : nullptr);
+                if (j == (kLag == 1 ? 2 : kChunks - 1)) {
                     fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(sum_empty(done & 1));
                 }
             }
-            if (kLag != 1) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(sum_empty(done & 1));
-            }
         }
     }
 
-    if (split > 1) {  // one tile to a cluster: each block adds a share of its elements, in the order of k
-        __syncwarp();
-        cluster_sync();
-        const int64_t row0 = int64_t(first % p.m_tiles) * NT;
-        const int rows = static_cast<int>(min(int64_t(NT), p.m - row0)), n0 = first / p.m_tiles * kRows;
-        const int total = rows * kRows;
-        for (int e = part * kThreads + threadIdx.x; e < total; e += split * kThreads) {
-            float v = 0.0f;
-            for (int r = 0; r < split; ++r) v += cluster_load(ring + 4 * e, r);
-            const int64_t col = int64_t(n0) + e % kRows;
-            if (col < p.n) {
-                T *at = static_cast<T *>(p.c) + (row0 + e / kRows) * p.ldc + col;
-                v *= p.alpha;
-                if (p.beta != 0.0f) v += p.beta * to_float(*at);
-                *at = from_float<T>(v);
-            }
-        }
-        cluster_sync();  // no block leaves while others read its sums
-    }
+    if (*failed) let_copies_land();
+    if (split > 1)  // one tile to a cluster
+        join_split(out, ring, 0, 1, part, split, int64_t(first % p.m_tiles) * NT, int64_t(first / p.m_tiles) * kRows, NT);
     fence_before();
     __syncthreads();
     if (warp == 5) {
@@ -241,22 +187,18 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     using S = Shape<NT>;
     const int64_t nb = mx_blocks(A.cols);
     CUtensorMap a_map, b_map;
-    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, NT);
-    if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows);
+    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, NT, true);
+    if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows, true);
     if (e != cudaSuccess) return e;
     Params p;
     p.a_scales = static_cast<const uint8_t *>(A.scales);
     p.b_scales = static_cast<const uint8_t *>(B.scales);
-    p.c = C.ptr;
-    p.ldc = C.ld;
     p.m = C.rows;
-    p.n = C.cols;
     p.steps = static_cast<int>(mx_ceil(nb, 2));
     p.scale_tiles = static_cast<int>(mx_scale_tiles(A.cols));
     p.n_tiles = static_cast<int>(mx_ceil(C.cols, kRows));
     p.m_tiles = static_cast<int>(mx_ceil(C.rows, NT));
-    p.alpha = alpha;
-    p.beta = beta;
+    const Output<T> out{static_cast<T *>(C.ptr), C.ld, C.rows, C.cols, alpha, beta};
     const int64_t tiles = int64_t(p.n_tiles) * p.m_tiles;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     const int stages_k = (p.steps + 3) / 4;
@@ -274,7 +216,7 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     cfg.numAttrs = 1;
     e = cudaFuncSetAttribute(product_kernel<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
     if (e != cudaSuccess) return e;
-    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, p, split);
+    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, p, out, split);
     if (e == cudaSuccess) count_launch();
     return e;
 }

@@ -31,6 +31,17 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// An arrival at the same barrier of another block of the cluster.  What it
+// announces is read by tensor cores, not by threads: the writer's
+// fence.proxy.async (or tcgen05 fence) before it orders that, and a release at
+// cluster scope would only stall the warp (measured: 2000 cycles each).
+__device__ __forceinline__ void bar_arrive_at(uint32_t bar, uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar),
+        "r"(rank)
+        : "memory");
+}
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t p;
     asm volatile(
@@ -44,8 +55,8 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 // Every wait ends: after kWaitClocks (some seconds; the longest sound wait, for
 // the products over the largest k, is below) it gives up and marks the block as
 // failed, which ends the block's other waits too.  A failed block computes
-// nothing more, waits (as long at most) for its copies in flight, frees its
-// tensor memory and leaves; costa_mx_failures tells the host.
+// nothing more, lets its copies in flight land, frees its tensor memory and
+// leaves; costa_mx_failures tells the host.
 constexpr long long kWaitClocks = 8000000000ll;
 
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
@@ -59,12 +70,28 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return false;
 }
 
+// Some milliseconds, far longer than any copy in flight takes.
+__device__ __forceinline__ void let_copies_land() {
+    const long long start = clock64();
+    while (clock64() - start < 10000000) __nanosleep(1000);
+}
+
 // ---- copies into shared memory ----
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
         "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+// The same, counted at the barrier of block `rank` (of this pair of blocks).
+__device__ __forceinline__ void tma_load_2d_at(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar,
+                                               uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\t"
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+        "%3}], [a];\n\t}" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar), "r"(rank)
         : "memory");
 }
 // bytes: a multiple of 16; both addresses 16-byte aligned
@@ -81,6 +108,14 @@ __device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols) {  // 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
 }
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t *slot, uint32_t cols) {  // one warp of each block
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
 }
@@ -88,6 +123,13 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// To the barriers of the blocks in `mask` (bits are ranks in the cluster).
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint32_t mask) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     bar),
+                 "h"(static_cast<uint16_t>(mask))
+                 : "memory");
 }
 // 16 columns of this warp's 32 lanes, one lane to a thread
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
@@ -132,7 +174,30 @@ __device__ __forceinline__ constexpr uint32_t idesc_e2m1(int n, int half) {
            uint32_t(half) << 29;
 }
 
-// ---- clusters ----
+// D[256 x n] += A B^T over 16 elements of bf16, both operands MN-major, by a
+// pair of blocks: each holds 128 rows of A and of D, and half of B's rows.
+__device__ __forceinline__ void mma_bf16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+        : "memory");
+}
+// bf16 x bf16 to f32, 256 rows, both operands MN-major.
+__device__ __forceinline__ constexpr uint32_t idesc_bf16_pair(int n) {
+    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | uint32_t(n >> 3) << 17 | uint32_t(256 >> 4) << 24;
+}
+
+// ---- registers and clusters ----
+
+// More (or fewer) registers for each thread of this warpgroup, from those that
+// the block was launched with.
+template <int N> __device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N> __device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -150,6 +215,60 @@ __device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
     return v;
 }
 
-}  // namespace mx
+// ---- the way out of tensor memory ----
 
+// An output of row-major rows, `rows` x `cols`: out = alpha sum + beta out.
+template <typename T> struct Output {
+    T *p;
+    int64_t ld, rows, cols;
+    float alpha, beta;
+    __device__ void put(int64_t row, int64_t col, float sum) const {
+        T *at = p + row * ld + col;
+        float v = alpha * sum;
+        if (beta != 0.0f) v += beta * to_float(*at);
+        *at = from_float<T>(v);
+    }
+};
+
+// Columns 16 ch .. 16 ch + 15 of a tile's sums: rows of the output from row0
+// (the tile's first), each warp's lanes at neighbouring columns from col0.
+// With `part` not null they are kept there instead, 128 to a row.
+template <typename T>
+__device__ __forceinline__ void tile_out16(const Output<T> &out, uint32_t tmem, int ch, int64_t row0, int64_t col0,
+                                           float *part) {
+    const int warp = threadIdx.x / 32 % 4, lane = threadIdx.x % 32;
+    const int64_t row = row0 + ch * 16, col = col0 + warp * 32 + lane;
+    if (row >= out.rows) return;
+    uint32_t r[16];
+    tmem_ld16(tmem + (uint32_t(warp * 32) << 16) + ch * 16, r);
+    tmem_wait_ld();
+    if (part) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part[(ch * 16 + i) * 128 + warp * 32 + lane] = __uint_as_float(r[i]);
+    } else if (col < out.cols) {
+        const int rows = static_cast<int>(min(int64_t(16), out.rows - row));
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < rows) out.put(row + i, col, __uint_as_float(r[i]));
+    }
+}
+
+// Joins the partial sums of `split` blocks of a cluster (at shared address
+// `part` of the blocks first, first + step, ...), in that order; each of them,
+// the index-th, writes a share.  All threads of the cluster call this.
+template <typename T>
+__device__ __forceinline__ void join_split(const Output<T> &out, uint32_t part, int first, int step, int index, int split,
+                                           int64_t row0, int64_t col0, int tile_rows) {
+    __syncwarp();
+    cluster_sync();
+    const int total = static_cast<int>(min(int64_t(tile_rows), out.rows - row0)) * 128;
+    for (int e = index * blockDim.x + threadIdx.x; e < total; e += split * blockDim.x) {
+        float v = 0.0f;
+        for (int r = 0; r < split; ++r) v += cluster_load(part + 4 * e, first + r * step);
+        if (col0 + e % 128 < out.cols) out.put(row0 + e / 128, col0 + e % 128, v);
+    }
+    cluster_sync();  // no block leaves while others read its sums
+}
+
+}  // namespace mx
 }  // namespace costa

@@ -290,7 +290,8 @@ def test_act_nan(name):
 
 
 GRADS = [(1, 1, 1), (1, 128, 64), (3, 5, 33), (17, 129, 96), (31, 64, 257), (64, 64, 64), (65, 300, 100), (128, 256, 256),
-         (200, 130, 520), (777, 100, 153), (4100, 72, 40), (33, 1000, 24), (5000, 8, 300)]
+         (200, 130, 520), (777, 100, 153), (4100, 72, 40), (33, 1000, 24), (5000, 8, 300), (130, 5000, 2100),
+         (200, 5000, 2600)]
 
 
 @pytest.mark.parametrize("m, n, k", GRADS)
