@@ -16,11 +16,10 @@ __device__ __forceinline__ float pow2(int biased) {
     return __uint_as_float(bits);
 }
 
-// The scale byte of a block from the bits of its largest magnitude: the
-// exponent field is floor(log2) + 127 for normal numbers; subnormal ones and
-// zero clamp to 0, where their field already is.  255: an infinity or a NaN.
-template <int FMT> __device__ __forceinline__ int scale_byte(uint32_t amax) {
-    const int e = static_cast<int>(amax >> 23);
+// The scale byte of a block from the biased exponent of its largest magnitude:
+// floor(log2) + 127 for normal numbers; subnormal ones and zero clamp to 0, where
+// their exponent field already is.  255: an infinity or a NaN.
+template <int FMT> __device__ __forceinline__ int scale_byte(int e) {
     if (e == 255) return 255;
     return FMT == COSTA_MX_E2M1 ? max(e - 2, 0) : e;
 }
@@ -34,19 +33,37 @@ __device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
     return r;
 }
 
-// What takes an element to its code's range for scale byte s (not 255): every
-// factor is a normal power of two, so the products are exact unless they are
-// below the smallest subnormal, far below half of the least code.
-struct ToE2M1 {
-    float f;
-    __device__ explicit ToE2M1(int s) : f(pow2(254 - s)) {}  // s <= 252
-    __device__ float operator()(float x) const { return x * f; }
-};
-struct ToI8 {
-    float c, f;  // x 2^(6 - E); for the smallest scales that factor is beyond a float
-    __device__ explicit ToI8(int s) : c(s < 6 ? 64.0f : 1.0f), f(pow2(s < 6 ? 254 - s : 260 - s)) {}
-    __device__ int operator()(float x) const { return max(-127, min(127, __float2int_rn(x * c * f))); }
-};
+// Codes of 8 elements x(0) .. x(7), for scale byte s; zero codes for 255.  What
+// takes an element to its code's range is a normal power of two (two of them
+// for I8 below 2^-121, where 2^(6 - E) is beyond a float), so the products are
+// exact unless they are subnormal, far below half of the least code.
+template <typename X> __device__ __forceinline__ uint32_t e2m1_of8(const X &x, int s) {
+    if (s == 255) return 0;
+    const float f = pow2(254 - s);  // s <= 252
+    return e2m1x2(x(0) * f, x(1) * f) | e2m1x2(x(2) * f, x(3) * f) << 8 | e2m1x2(x(4) * f, x(5) * f) << 16 |
+           e2m1x2(x(6) * f, x(7) * f) << 24;
+}
+
+// Added to 1.5 2^23 a number below 2^22 is rounded to an integer, to nearest
+// even, in the low bits; they are clamped in pairs of 16 bits.
+__device__ __forceinline__ uint32_t i8_of4(float a, float b, float c, float d, float f) {
+    constexpr float kRound = 12582912.0f;
+    uint32_t p = __byte_perm(__float_as_uint(fmaf(a, f, kRound)), __float_as_uint(fmaf(b, f, kRound)), 0x5410);
+    uint32_t q = __byte_perm(__float_as_uint(fmaf(c, f, kRound)), __float_as_uint(fmaf(d, f, kRound)), 0x5410);
+    p = __vmaxs2(__vmins2(p, 0x007f007fu), 0xff81ff81u);
+    q = __vmaxs2(__vmins2(q, 0x007f007fu), 0xff81ff81u);
+    return __byte_perm(p, q, 0x6420);
+}
+template <typename X> __device__ __forceinline__ uint2 i8_of8(const X &x, int s) {
+    if (s == 255) return make_uint2(0, 0);
+    if (s >= 6) {
+        const float f = pow2(260 - s);
+        return make_uint2(i8_of4(x(0), x(1), x(2), x(3), f), i8_of4(x(4), x(5), x(6), x(7), f));
+    }
+    const float f = pow2(254 - s);
+    return make_uint2(i8_of4(x(0) * 64.0f, x(1) * 64.0f, x(2) * 64.0f, x(3) * 64.0f, f),
+                      i8_of4(x(4) * 64.0f, x(5) * 64.0f, x(6) * 64.0f, x(7) * 64.0f, f));
+}
 
 // The value of an I8 code for scale byte s is q times this: 2^(s - 133), below 2^-126 for small s.
 __device__ __forceinline__ float i8_unit(int s) {
@@ -54,41 +71,20 @@ __device__ __forceinline__ float i8_unit(int s) {
     return __uint_as_float(bits);
 }
 
-// Codes of 8 elements (4 or 8 bytes), for scale byte s; zero codes for 255.
-__device__ __forceinline__ uint32_t e2m1_of8(const float (&x)[8], int s) {
-    if (s == 255) return 0;
-    const ToE2M1 to(s);
-    return e2m1x2(to(x[0]), to(x[1])) | e2m1x2(to(x[2]), to(x[3])) << 8 | e2m1x2(to(x[4]), to(x[5])) << 16 |
-           e2m1x2(to(x[6]), to(x[7])) << 24;
-}
-__device__ __forceinline__ uint2 i8_of8(const float (&x)[8], int s) {
-    if (s == 255) return make_uint2(0, 0);
-    const ToI8 to(s);
-    uint32_t w[2];
+// Values of 4 codes of E2M1 (the low 16 bits) and of I8.  The three low bits of
+// an E2M1 code are the exponent and fraction of a float 2^126 times smaller (0.5
+// a subnormal one); an I8 code q is taken as the float 2^23 + 128 + q.
+__device__ __forceinline__ void e2m1_to4(uint32_t codes, float unit, float (&v)[4]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        w[h] = __byte_perm(__byte_perm(to(x[4 * h]), to(x[4 * h + 1]), 0x0040),
-                           __byte_perm(to(x[4 * h + 2]), to(x[4 * h + 3]), 0x0040), 0x5410);
-    return make_uint2(w[0], w[1]);
-}
-
-// Values of 8 codes.
-__device__ __forceinline__ void e2m1_to8(uint32_t codes, float unit, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t c = codes >> (4 * i);
-        // exponent 1 .. 3 with one fraction bit, or 0 / 0.5: 2 |v| as an integer, 0 1 2 3 4 6 8 12
-        const int twice = (0xC8643210u >> (4 * (c & 7))) & 15;
-        const float m = 0.5f * unit * static_cast<float>(twice);
-        v[i] = c & 8 ? -m : m;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t top = codes << (28 - 4 * i);  // the code in the top four bits
+        v[i] = __uint_as_float((top & 0x80000000u) | (top >> 6 & 0x01c00000u)) * 0x1p126f * unit;
     }
 }
-__device__ __forceinline__ void i8_to8(uint2 codes, float unit, float (&v)[8]) {
+__device__ __forceinline__ void i8_to4(uint32_t codes, float unit, float (&v)[4]) {
+    const uint32_t w = codes ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t w = i < 4 ? codes.x : codes.y;
-        v[i] = unit * static_cast<float>(static_cast<int8_t>(w >> (8 * (i & 3))));
-    }
+    for (int i = 0; i < 4; ++i) v[i] = unit * (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7540 | i)) - 8388736.0f);
 }
 
 // Byte of block j of row i in E2M1's scales.
@@ -128,23 +124,6 @@ __device__ __forceinline__ void load8(const T *row, int64_t col, int64_t cols, b
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T *row, int64_t col, int64_t cols, bool vec, const float (&x)[8]) {
-    if (vec && col + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(row + col) = make_float4(x[0], x[1], x[2], x[3]);
-            *reinterpret_cast<float4 *>(row + col + 4) = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-            *reinterpret_cast<uint4 *>(row + col) =
-                make_uint4(bf16x2(x[0], x[1]), bf16x2(x[2], x[3]), bf16x2(x[4], x[5]), bf16x2(x[6], x[7]));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = from_float<T>(x[i]);
-    }
 }
 
 }  // namespace mx

@@ -12,36 +12,189 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Rows cut into groups of 8 elements, one to a thread; 4 lanes share a block.
-// gpr: groups of a row, a multiple of 4 (a block's lanes lie in one warp).
+// Rows cut into groups of 16 elements, half a block, one to a thread: two
+// neighbouring lanes share a block, a warp takes 16 of them.  gpr: groups of a
+// row, even (so a block's lanes lie in one warp).
 struct Groups {
     int64_t gpr, total;
-    __device__ bool at(int64_t &row, int64_t &col) const {
+    uint32_t mul, shift;  // x / gpr = (x mul >> 32) >> shift for x < 2^31
+    // This thread's group; past the last one a place without elements (col = none).
+    __device__ bool at(int64_t none, int64_t &row, int64_t &col) const {
         const int64_t g = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+        row = 0;
+        col = none;
+        if (g >= total) return false;
         if (total <= 0x7fffffff) {
-            const uint32_t r = static_cast<uint32_t>(g) / static_cast<uint32_t>(gpr);
+            const uint32_t r = __umulhi(static_cast<uint32_t>(g), mul) >> shift;
             row = r;
-            col = (static_cast<uint32_t>(g) - r * static_cast<uint32_t>(gpr)) * 8;
+            col = (static_cast<uint32_t>(g) - r * static_cast<uint32_t>(gpr)) * 16;
         } else {
             row = g / gpr;
-            col = (g - row * gpr) * 8;
+            col = (g - row * gpr) * 16;
         }
-        return g < total;
+        return true;
     }
 };
+
+Groups groups_of(int64_t rows, int64_t gpr) {
+    Groups g{gpr, rows * gpr, 0, 0};
+    if (g.total > 0x7fffffff) return g;
+    // 2^(s-1) < gpr <= 2^s and gpr even, so s >= 1: ceil(2^(31+s) / gpr) < 2^32 is exact for 31 bits
+    uint32_t s = 1;
+    while ((int64_t(1) << s) < gpr) ++s;
+    g.mul = static_cast<uint32_t>(((uint64_t(1) << (31 + s)) + gpr - 1) / gpr);
+    g.shift = s - 1;
+    return g;
+}
 
 unsigned blocks_for(const Groups &g) { return static_cast<unsigned>(mx_ceil(g.total, kThreads)); }
 
 template <typename T> struct Dense {
     T *p;
     int64_t ld;
-    bool vec;  // rows start on 16-byte boundaries
+    int align;  // rows start on boundaries of 32 bytes (2), of 16 (1) or any (0)
 };
 
 template <typename T> Dense<T> dense(const costa_mx_dense &d) {
-    return {static_cast<T *>(d.ptr), d.ld,
-            reinterpret_cast<uint64_t>(d.ptr) % 16 == 0 && (d.ld * static_cast<int64_t>(sizeof(T))) % 16 == 0};
+    const uint64_t bits = reinterpret_cast<uint64_t>(d.ptr) | static_cast<uint64_t>(d.ld) * sizeof(T);
+    return {static_cast<T *>(d.ptr), d.ld, bits % 32 == 0 ? 2 : bits % 16 == 0 ? 1 : 0};
 }
+
+// 16 elements as they lie in memory.
+template <typename T> struct Sixteen;
+template <> struct Sixteen<float> {
+    uint32_t w[16];
+    __device__ float operator()(int i) const { return __uint_as_float(w[i]); }
+    __device__ void set(int i, float x) { w[i] = __float_as_uint(x); }
+    __device__ int exponent() const {  // biased, of the largest magnitude
+        uint32_t a = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a = max(a, w[i] & 0x7fffffffu);
+        return a >> 23;
+    }
+};
+template <> struct Sixteen<__nv_bfloat16> {
+    uint32_t w[8];
+    __device__ float operator()(int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+    __device__ void set(int i, float x) {  // in order: a whole word at odd i
+        if (i % 2 == 0)
+            w[i / 2] = __float_as_uint(x);
+        else
+            w[i / 2] = bf16x2(__uint_as_float(w[i / 2]), x);
+    }
+    __device__ int exponent() const {
+        uint32_t a = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a = __vmaxu2(a, w[i] & 0x7fff7fffu);
+        return max(a & 0xffffu, a >> 16) >> 7;
+    }
+};
+
+// 32 bytes at a 32-byte boundary
+__device__ __forceinline__ void load32(const void *p, uint32_t *w) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t *w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
+// The elements of a warp's 32 groups where rows are not aligned or end inside a
+// group: the lanes take a block's 32 elements together, through 2 KB of shared
+// memory of the warp.  Lane 2 i holds block i's place and how many of its
+// elements exist.
+struct Blocks {
+    int64_t place;
+    int count;
+    __device__ Blocks(int64_t row, int64_t col, int64_t cols, int64_t ld)
+        : place(row * ld + col), count(static_cast<int>(max(int64_t(0), min(int64_t(32), cols - col)))) {}
+    __device__ int64_t place_of(int i) const { return __shfl_sync(~0u, place, 2 * i); }
+    __device__ int count_of(int i) const { return __shfl_sync(~0u, count, 2 * i); }
+};
+
+// This thread's 16 elements, 0 past the row's end.  Whole warps call this.
+template <typename T>
+__device__ __forceinline__ void get(const Dense<const T> &X, int64_t row, int64_t col, int64_t cols, float *stage,
+                                    Sixteen<T> &x) {
+    constexpr int kWords = sizeof(x.w) / 4;
+    if (X.align && __all_sync(~0u, col + 16 <= cols || col >= cols)) {
+        if (col >= cols) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) x.w[i] = 0;
+            return;
+        }
+        const T *p = X.p + row * X.ld + col;
+        if (X.align == 2) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8) load32(reinterpret_cast<const char *>(p) + 4 * i, x.w + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4)
+                *reinterpret_cast<uint4 *>(x.w + i) = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
+        }
+        return;
+    }
+    const int lane = threadIdx.x % 32;
+    const Blocks b(row, col, cols, X.ld);
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 16; h += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t place = b.place_of(h + i);
+            v[i] = lane < b.count_of(h + i) ? to_float(X.p[place + lane]) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) stage[32 * (h + i) + lane] = v[i];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        const float4 v = reinterpret_cast<const float4 *>(stage)[4 * lane + i / 4];
+        x.set(i, v.x);
+        x.set(i + 1, v.y);
+        x.set(i + 2, v.z);
+        x.set(i + 3, v.w);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void put(const Dense<T> &Y, int64_t row, int64_t col, int64_t cols, float *stage,
+                                    const Sixteen<T> &x) {
+    constexpr int kWords = sizeof(x.w) / 4;
+    if (Y.align && __all_sync(~0u, col + 16 <= cols || col >= cols)) {
+        if (col >= cols) return;
+        char *p = reinterpret_cast<char *>(Y.p + row * Y.ld + col);
+        if (Y.align == 2) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8) store32(p + 4 * i, x.w + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) *reinterpret_cast<uint4 *>(p + 4 * i) = *reinterpret_cast<const uint4 *>(x.w + i);
+        }
+        return;
+    }
+    const int lane = threadIdx.x % 32;
+    const Blocks b(row, col, cols, Y.ld);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+        reinterpret_cast<float4 *>(stage)[4 * lane + i / 4] = make_float4(x(i), x(i + 1), x(i + 2), x(i + 3));
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int64_t place = b.place_of(i);
+        if (lane < b.count_of(i)) Y.p[place + lane] = from_float<T>(stage[32 * i + lane]);
+    }
+}
+
+#define COSTA_MX_STAGE                                        \
+    __shared__ __align__(16) float stages[kThreads / 32][512]; \
+    float *const stage = stages[threadIdx.x / 32]
 
 struct Codes {
     uint8_t *codes, *scales;
@@ -54,174 +207,241 @@ Codes codes(const costa_mx_matrix &q) {
             q.format == COSTA_MX_E2M1 ? mx_scale_tiles(q.cols) : mx_scale_pitch(q.cols)};
 }
 
-// The largest magnitude of a block whose 32 elements 4 neighbouring lanes hold.
-__device__ __forceinline__ uint32_t block_amax(const float (&x)[8], unsigned lanes) {
-    uint32_t a = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, magnitude(x[i]));
-    a = max(a, __shfl_xor_sync(lanes, a, 1));
-    return max(a, __shfl_xor_sync(lanes, a, 2));
+// Writes the codes of 16 elements at (row, col) and returns the block's scale
+// byte; whole warps call this.  Only columns of existing blocks are written.
+template <int FMT, typename T>
+__device__ __forceinline__ int put_codes(const Codes &q, bool in, int64_t row, int64_t col, int64_t cols,
+                                         const Sixteen<T> &x) {
+    const int e = x.exponent();
+    const int s = scale_byte<FMT>(max(e, __shfl_xor_sync(~0u, e, 1)));
+    if (in && col < ((cols + 31) & ~int64_t(31))) {
+        auto low = [&](int i) { return x(i); };
+        auto high = [&](int i) { return x(i + 8); };
+        if constexpr (FMT == COSTA_MX_E2M1) {
+            *reinterpret_cast<uint2 *>(q.codes + row * q.ld + col / 2) = make_uint2(e2m1_of8(low, s), e2m1_of8(high, s));
+        } else {
+            const uint2 a = i8_of8(low, s), b = i8_of8(high, s);
+            *reinterpret_cast<uint4 *>(q.codes + row * q.ld + col) = make_uint4(a.x, a.y, b.x, b.y);
+        }
+    }
+    return s;
 }
 
-// Writes the codes of 8 elements at (row, col) and, by the block's first lane,
-// the scale.  E2M1: `col` may lie in the padding of the last scale tile.
-template <int FMT>
-__device__ __forceinline__ void put8(const Codes &q, int64_t row, int64_t col, int64_t cols, const float (&x)[8],
-                                     unsigned lanes) {
-    const int s = scale_byte<FMT>(block_amax(x, lanes));
-    const bool inside = col < ((cols + 31) & ~int64_t(31));
-    if constexpr (FMT == COSTA_MX_E2M1) {
-        if (inside) *reinterpret_cast<uint32_t *>(q.codes + row * q.ld + col / 2) = e2m1_of8(x, s);
-        if ((col & 31) == 0) q.scales[scale_at(row, col >> 5, q.unit)] = static_cast<uint8_t>(s);
-    } else {
-        if (inside) *reinterpret_cast<uint2 *>(q.codes + row * q.ld + col) = i8_of8(x, s);
-        if (inside && (col & 31) == 0) q.scales[row * q.unit + (col >> 5)] = static_cast<uint8_t>(s);
-    }
+// The same with the scale.  E2M1: `col` may lie in the padding of the last scale tile.
+template <int FMT, typename T>
+__device__ __forceinline__ void put16(const Codes &q, bool in, int64_t row, int64_t col, int64_t cols,
+                                      const Sixteen<T> &x) {
+    const int s = put_codes<FMT>(q, in, row, col, cols, x);
+    if (!in || (col & 31) != 0) return;
+    if constexpr (FMT == COSTA_MX_E2M1)
+        q.scales[scale_at(row, col >> 5, q.unit)] = static_cast<uint8_t>(s);
+    else
+        q.scales[row * q.unit + (col >> 5)] = static_cast<uint8_t>(s);
 }
 
-template <int FMT>
-__device__ __forceinline__ void get8(const Codes &q, int64_t row, int64_t col, float (&v)[8]) {
-    if constexpr (FMT == COSTA_MX_E2M1) {
-        const float unit = pow2(q.scales[scale_at(row, col >> 5, q.unit)]);
-        e2m1_to8(*reinterpret_cast<const uint32_t *>(q.codes + row * q.ld + col / 2), unit, v);
-    } else {
-        const float unit = i8_unit(q.scales[row * q.unit + (col >> 5)]);
-        i8_to8(*reinterpret_cast<const uint2 *>(q.codes + row * q.ld + col), unit, v);
+// 16 codes and what they are multiples of.
+template <int FMT> struct Coded {
+    uint32_t w[FMT == COSTA_MX_E2M1 ? 2 : 4];
+    float unit;
+    __device__ void load(const Codes &q, int64_t row, int64_t col) {
+        if constexpr (FMT == COSTA_MX_E2M1) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(q.codes + row * q.ld + col / 2);
+            w[0] = v.x;
+            w[1] = v.y;
+            unit = pow2(q.scales[scale_at(row, col >> 5, q.unit)]);
+        } else {
+            const uint4 v = *reinterpret_cast<const uint4 *>(q.codes + row * q.ld + col);
+            w[0] = v.x;
+            w[1] = v.y;
+            w[2] = v.z;
+            w[3] = v.w;
+            unit = i8_unit(q.scales[row * q.unit + (col >> 5)]);
+        }
     }
-}
+    __device__ void four(int i, float (&v)[4]) const {  // values of codes 4 i .. 4 i + 3
+        if constexpr (FMT == COSTA_MX_E2M1)
+            e2m1_to4(w[i / 2] >> (i % 2 * 16), unit, v);
+        else
+            i8_to4(w[i], unit, v);
+    }
+};
 
 // Groups of a row of codes: whole blocks, and for E2M1 whole scale tiles.
 Groups groups(const costa_mx_matrix &q, bool tiles) {
-    const int64_t gpr = tiles && q.format == COSTA_MX_E2M1 ? mx_scale_tiles(q.cols) * 16 : mx_blocks(q.cols) * 4;
-    return {gpr, q.rows * gpr};
+    return groups_of(q.rows,
+                     tiles && q.format == COSTA_MX_E2M1 ? mx_scale_tiles(q.cols) * 8 : mx_blocks(q.cols) * 2);
 }
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) quantize_n_kernel(Dense<const T> X, Codes Q, int64_t cols, Groups gr) {
+    COSTA_MX_STAGE;
     int64_t row, col;
-    const bool in = gr.at(row, col);
-    const unsigned lanes = __ballot_sync(~0u, in);
-    if (!in) return;
-    float x[8];
-    load8(X.p + row * X.ld, col, cols, X.vec, x);
-    put8<FMT>(Q, row, col, cols, x, lanes);
+    const bool in = gr.at(cols, row, col);
+    Sixteen<T> x;
+    get(X, row, col, cols, stage, x);
+    put16<FMT>(Q, in, row, col, cols, x);
 }
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> Y, int64_t cols, Groups gr) {
+    COSTA_MX_STAGE;
     int64_t row, col;
-    if (!gr.at(row, col)) return;
-    float v[8];
-    get8<FMT>(Q, row, col, v);
-    store8(Y.p + row * Y.ld, col, cols, Y.vec, v);
+    Coded<FMT> q;
+    if (gr.at(cols, row, col)) q.load(Q, row, col);
+    Sixteen<T> y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[4];
+        q.four(i, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y.set(4 * i + j, v[j]);
+    }
+    put(Y, row, col, cols, stage, y);
 }
 
 // Quantisation across rows: a block is 32 rows of one column, which one thread
-// holds.  A thread block takes 256 rows x 64 columns; a warp 32 rows, two
-// columns to a lane.  The codes go through shared memory so that each column's
-// 8 blocks (128 or 256 bytes of a row of QT) are written together.
-constexpr int kTRows = 256, kTCols = 64;
+// holds.  A thread block takes 128 rows x 128 columns, which is a tile of
+// E2M1's scales in either order; a warp 32 rows x 64 columns, two to a lane
+// (neighbours where bf16 rows are 4-byte aligned, else 32 apart).  The codes go
+// through shared memory so that each column's 4 blocks (64 or 128 bytes of a
+// row of QT) are written together.  Neighbouring thread blocks take
+// neighbouring columns, for the memory's pages.  With BOTH the same rows are
+// then read again, from the cache, 8 lanes to a row.
+constexpr int kTile = 128;
 
 template <typename T, int FMT, bool BOTH>
-__global__ void __launch_bounds__(kThreads) quantize_t_kernel(Dense<const T> X, int64_t rows, int64_t cols, Codes QN,
-                                                              Codes QT, unsigned row_tiles) {
-    constexpr int kBlockBytes = FMT == COSTA_MX_E2M1 ? 16 : 32, kPitch = 8 * kBlockBytes + 16;
-    __shared__ __align__(16) uint8_t stage[kTCols * kPitch];
-    __shared__ uint8_t sc[kTCols][8];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int64_t r0 = int64_t(blockIdx.x % row_tiles) * kTRows, c0 = int64_t(blockIdx.x / row_tiles) * kTCols;
-    const int64_t rw = r0 + warp * 32, c = c0 + 2 * lane;
+__global__ void __launch_bounds__(kThreads, 2) quantize_t_kernel(Dense<const T> X, bool pairs, int64_t rows, int64_t cols,
+                                                                 Codes QN, Codes QT, unsigned col_tiles) {
+    constexpr int kBlockBytes = FMT == COSTA_MX_E2M1 ? 16 : 32, kPitch = 4 * kBlockBytes + 16;
+    __shared__ __align__(16) uint8_t codes[kTile * kPitch];
+    __shared__ __align__(16) uint8_t sc[2][kTile][4];
+    COSTA_MX_STAGE;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, block = warp % 4, left = warp / 4 * 64;
+    const int64_t r0 = int64_t(blockIdx.x / col_tiles) * kTile, c0 = int64_t(blockIdx.x % col_tiles) * kTile;
     float x[2][32];
-    const bool pair = X.vec && c + 2 <= cols;
+    if (sizeof(T) == 2 && pairs) {
+        const int64_t c = c0 + left + 2 * lane;
+        const T *p = X.p + (r0 + 32 * block) * X.ld + c;
+        uint32_t v[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const T *p = X.p + (rw + i) * X.ld + c;
-        x[0][i] = x[1][i] = 0.0f;
-        if (rw + i < rows) {
-            if (pair) {
-                if constexpr (sizeof(T) == 4) {
-                    const float2 v = *reinterpret_cast<const float2 *>(p);
-                    x[0][i] = v.x;
-                    x[1][i] = v.y;
-                } else {
-                    const uint32_t v = *reinterpret_cast<const uint32_t *>(p);
-                    x[0][i] = __uint_as_float(v << 16);
-                    x[1][i] = __uint_as_float(v & 0xffff0000u);
-                }
-            } else {
-                if (c < cols) x[0][i] = to_float(p[0]);
-                if (c + 1 < cols) x[1][i] = to_float(p[1]);
-            }
+        for (int i = 0; i < 32; ++i) {
+            const bool in = r0 + 32 * block + i < rows;
+            v[i] = 0;
+            if (in && c + 1 < cols)
+                v[i] = *reinterpret_cast<const uint32_t *>(p + i * X.ld);
+            else if (in && c < cols)
+                v[i] = *reinterpret_cast<const uint16_t *>(p + i * X.ld);
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            x[0][i] = __uint_as_float(v[i] << 16);
+            x[1][i] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t c = c0 + left + lane + 32 * h;
+            const T *p = X.p + (r0 + 32 * block) * X.ld + c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[h][i] = c < cols && r0 + 32 * block + i < rows ? to_float(p[i * X.ld]) : 0.0f;
         }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+        const int col = left + (sizeof(T) == 2 && pairs ? 2 * lane + h : lane + 32 * h);
         uint32_t a = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) a = max(a, magnitude(x[h][i]));
-        const int s = scale_byte<FMT>(a);
-        uint8_t *to = stage + (2 * lane + h) * kPitch + warp * kBlockBytes;
-        sc[2 * lane + h][warp] = static_cast<uint8_t>(s);
+        const int s = scale_byte<FMT>(a >> 23);
+        uint8_t *to = codes + col * kPitch + block * kBlockBytes;
+        sc[0][col][block] = static_cast<uint8_t>(s);
+        uint32_t w[kBlockBytes / 4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            float y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[h][8 * k + i];
-            if constexpr (FMT == COSTA_MX_E2M1)
-                *reinterpret_cast<uint32_t *>(to + 4 * k) = e2m1_of8(y, s);
-            else
-                *reinterpret_cast<uint2 *>(to + 8 * k) = i8_of8(y, s);
+            auto y = [&](int i) { return x[h][8 * k + i]; };
+            if constexpr (FMT == COSTA_MX_E2M1) {
+                w[k] = e2m1_of8(y, s);
+            } else {
+                const uint2 u = i8_of8(y, s);
+                w[2 * k] = u.x;
+                w[2 * k + 1] = u.y;
+            }
         }
+#pragma unroll
+        for (int k = 0; k < kBlockBytes / 16; ++k)
+            reinterpret_cast<uint4 *>(to)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
     }
     __syncthreads();
     const int64_t nb = (rows + 31) >> 5, b0 = r0 >> 5;  // blocks of a row of QT; the first of these
-    constexpr int kChunks = 8 * kBlockBytes / 16;       // 16-byte pieces of a column's codes
-    for (int k = threadIdx.x; k < kTCols * kChunks; k += kThreads) {
-        const int col = k / kChunks, piece = k % kChunks;
+    constexpr int kChunks = 4 * kBlockBytes / 16;       // 16-byte pieces of a column's codes
+#pragma unroll
+    for (int j = 0; j < kTile * kChunks / kThreads; ++j) {
+        const int k = j * kThreads + threadIdx.x, col = k / kChunks, piece = k % kChunks;
         if (c0 + col < cols && b0 + piece * 16 / kBlockBytes < nb)
             *reinterpret_cast<uint4 *>(QT.codes + (c0 + col) * QT.ld + b0 * kBlockBytes + piece * 16) =
-                *reinterpret_cast<const uint4 *>(stage + col * kPitch + piece * 16);
+                *reinterpret_cast<const uint4 *>(codes + col * kPitch + piece * 16);
     }
-    for (int k = threadIdx.x; k < kTCols * 8; k += kThreads) {
-        const int col = k / 8;
-        const int64_t b = b0 + k % 8;
-        if (c0 + col >= cols) continue;
+    // The 4 scales of row `row` of a matrix of codes of `q_rows` x `q_cols`, from `from`.
+    auto put_scales = [](const Codes &q, int64_t row, int64_t q_rows, int64_t q_cols, int64_t first, const uint8_t *from) {
+        if (row >= q_rows) return;
         if constexpr (FMT == COSTA_MX_E2M1) {
-            if (b < QT.unit * 4) QT.scales[scale_at(c0 + col, b, QT.unit)] = sc[col][k % 8];
+            *reinterpret_cast<uint32_t *>(q.scales + scale_at(row, first, q.unit)) = *reinterpret_cast<const uint32_t *>(from);
         } else {
-            if (b < nb) QT.scales[(c0 + col) * QT.unit + b] = sc[col][k % 8];
+            uint8_t *to = q.scales + row * q.unit + first;
+            const int64_t left_over = ((q_cols + 31) >> 5) - first;
+            if (left_over >= 4)
+                *reinterpret_cast<uint32_t *>(to) = *reinterpret_cast<const uint32_t *>(from);
+            else
+                for (int64_t i = 0; i < left_over; ++i) to[i] = from[i];
         }
-    }
-    if constexpr (BOTH) {  // the same rows again, along the columns: 8 lanes to a row (read from the cache)
-#pragma unroll 4
-        for (int i = 0; i < 32; i += 4) {
-            const int64_t row = rw + i + lane / 8, col = c0 + (lane % 8) * 8;
-            const bool in = row < rows && col < (FMT == COSTA_MX_E2M1 ? QN.unit * 128 : ((cols + 31) & ~int64_t(31)));
-            const unsigned lanes = __ballot_sync(~0u, in);
-            if (in) {
-                float y[8];
-                load8(X.p + row * X.ld, col, cols, X.vec, y);
-                put8<FMT>(QN, row, col, cols, y, lanes);
+    };
+    if (threadIdx.x < kTile) put_scales(QT, c0 + threadIdx.x, cols, rows, b0, sc[0][threadIdx.x]);
+    if constexpr (BOTH) {
+        const int64_t col = c0 + lane % 8 * 16;
+        Sixteen<T> y[2];
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int64_t row = r0 + 16 * warp + 4 * (i + k) + lane / 8;
+                get(X, min(row, rows - 1), row < rows ? col : cols, cols, stage, y[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int64_t row = r0 + 16 * warp + 4 * (i + k) + lane / 8;
+                const int s = put_codes<FMT>(QN, row < rows, row, col, cols, y[k]);
+                if (lane % 2 == 0) sc[1][row - r0][lane % 8 / 2] = static_cast<uint8_t>(s);
             }
         }
+        __syncthreads();
+        if (threadIdx.x < kTile) put_scales(QN, r0 + threadIdx.x, rows, cols, c0 >> 5, sc[1][threadIdx.x]);
     }
+}
+
+// 1 / (1 + e^-x) within 2^-22 + |x| 2^-23 of itself: nothing beside |x| 2^-20,
+// the unit of what uses it.  Beyond the range of e^-x it is 0 or 1.
+__device__ __forceinline__ float sigmoid(float x) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
 }
 
 // act(x) and act'(x).
 template <int ACT> __device__ __forceinline__ float act(float x) {
-    if constexpr (ACT == COSTA_MX_SILU) return x / (1.0f + expf(-x));
-    if constexpr (ACT == COSTA_MX_GELU) return x * normcdff(x);
+    if constexpr (ACT == COSTA_MX_SILU) return x * sigmoid(x);
+    if constexpr (ACT == COSTA_MX_GELU) return x * (0.5f + 0.5f * erff(x * 0.7071067811865476f));
     return x > 0.0f || x != x ? x : 0.0f;
 }
 template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, float &slope) {
     if constexpr (ACT == COSTA_MX_SILU) {
-        const float s = 1.0f / (1.0f + expf(-x));
+        const float s = sigmoid(x);
         y = x * s;
         slope = s * (1.0f + x * (1.0f - s));
     } else if constexpr (ACT == COSTA_MX_GELU) {
-        const float c = normcdff(x);
+        const float c = 0.5f + 0.5f * erff(x * 0.7071067811865476f);
         y = x * c;
-        slope = c + x * expf(-0.5f * x * x) * 0.3989422804014327f;
+        slope = c + x * __expf(-0.5f * x * x) * 0.3989422804014327f;
     } else {
         y = act<ACT>(x);
         slope = x != x ? x : x > 0.0f ? 1.0f : 0.0f;
@@ -231,44 +451,52 @@ template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, f
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
                                                                Codes QG, int64_t cols, Groups gr) {
+    COSTA_MX_STAGE;
     int64_t row, col;
-    const bool in = gr.at(row, col);
-    const unsigned lanes = __ballot_sync(~0u, in);
-    if (!in) return;
-    float x[8], g[8], y[8];
-    load8(X.p + row * X.ld, col, cols, X.vec, x);
-    if constexpr (GATED) load8(G.p + row * G.ld, col, cols, G.vec, g);
+    const bool in = gr.at(cols, row, col);
+    Sixteen<T> x, g, y;
+    get(X, row, col, cols, stage, x);
+    if constexpr (GATED) get(G, row, col, cols, stage, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i] = act<ACT>(x[i]);
-        if constexpr (GATED) y[i] *= g[i];
-    }
-    store8(Y.p + row * Y.ld, col, cols, Y.vec, y);
-    put8<COSTA_MX_I8>(QX, row, col, cols, x, lanes);
-    if constexpr (GATED) put8<COSTA_MX_I8>(QG, row, col, cols, g, lanes);
+    for (int i = 0; i < 16; ++i) y.set(i, GATED ? act<ACT>(x(i)) * g(i) : act<ACT>(x(i)));
+    put(Y, row, col, cols, stage, y);
+    put16<COSTA_MX_I8>(QX, in, row, col, cols, x);
+    if constexpr (GATED) put16<COSTA_MX_I8>(QG, in, row, col, cols, g);
 }
 
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
                                                                 Dense<T> dG, int64_t cols, Groups gr) {
+    COSTA_MX_STAGE;
     int64_t row, col;
-    if (!gr.at(row, col)) return;
-    float x[8], g[8], d[8], dg[8];
-    load8(dY.p + row * dY.ld, col, cols, dY.vec, d);
-    get8<COSTA_MX_I8>(QX, row, col, x);
-    if constexpr (GATED) get8<COSTA_MX_I8>(QG, row, col, g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float y, slope;
-        act_both<ACT>(x[i], y, slope);
-        if constexpr (GATED) {
-            dg[i] = d[i] * y;
-            d[i] *= g[i];
-        }
-        d[i] *= slope;
+    const bool in = gr.at(cols, row, col);
+    Sixteen<T> d, dx, dg;
+    Coded<COSTA_MX_I8> x, g;
+    if (in) {
+        x.load(QX, row, col);
+        if constexpr (GATED) g.load(QG, row, col);
     }
-    store8(dX.p + row * dX.ld, col, cols, dX.vec, d);
-    if constexpr (GATED) store8(dG.p + row * dG.ld, col, cols, dG.vec, dg);
+    get(dY, row, col, cols, stage, d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float xs[4], gs[4];
+        x.four(i, xs);
+        if constexpr (GATED) g.four(i, gs);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = 4 * i + j;
+            float y, slope;
+            act_both<ACT>(xs[j], y, slope);
+            if constexpr (GATED) {
+                dg.set(k, d(k) * y);
+                dx.set(k, d(k) * gs[j] * slope);
+            } else {
+                dx.set(k, d(k) * slope);
+            }
+        }
+    }
+    put(dX, row, col, cols, stage, dx);
+    if constexpr (GATED) put(dG, row, col, cols, stage, dg);
 }
 
 cudaError_t launched() {
@@ -305,16 +533,15 @@ cudaError_t backward(const costa_mx_matrix &QX, const costa_mx_matrix *QG, const
 
 template <typename T, int FMT>
 cudaError_t quantize_t(const costa_mx_dense &X, const costa_mx_matrix *QN, const costa_mx_matrix &QT, cudaStream_t s) {
-    const unsigned row_tiles = static_cast<unsigned>(mx_ceil(X.rows, kTRows));
-    // with QN also the columns that fill its last scale tile
-    const int64_t col_tiles = QN ? mx_scale_tiles(X.cols) * (128 / kTCols) : mx_ceil(X.cols, kTCols);
-    const unsigned grid = static_cast<unsigned>(row_tiles * col_tiles);
+    const unsigned col_tiles = static_cast<unsigned>(mx_ceil(X.cols, kTile));
+    const unsigned grid = static_cast<unsigned>(col_tiles * mx_ceil(X.rows, kTile));
+    const bool pairs = reinterpret_cast<uint64_t>(X.ptr) % 4 == 0 && X.ld % 2 == 0;
     if (QN)
         quantize_t_kernel<T, FMT, true>
-            <<<grid, kThreads, 0, s>>>(dense<const T>(X), X.rows, X.cols, codes(*QN), codes(QT), row_tiles);
+            <<<grid, kThreads, 0, s>>>(dense<const T>(X), pairs, X.rows, X.cols, codes(*QN), codes(QT), col_tiles);
     else
         quantize_t_kernel<T, FMT, false>
-            <<<grid, kThreads, 0, s>>>(dense<const T>(X), X.rows, X.cols, {}, codes(QT), row_tiles);
+            <<<grid, kThreads, 0, s>>>(dense<const T>(X), pairs, X.rows, X.cols, {}, codes(QT), col_tiles);
     return launched();
 }
 
