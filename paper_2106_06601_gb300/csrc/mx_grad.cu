@@ -91,18 +91,6 @@ __device__ __forceinline__ __nv_bfloat162 bf16_unit(uint32_t s) {
     return *reinterpret_cast<const __nv_bfloat162 *>(&two);
 }
 
-// A place in a ring of N stages and the parity of its barriers' current phase.
-template <int N> struct Ring {
-    int s = 0;
-    uint32_t parity = 0;
-    __device__ void next() {
-        if (++s == N) {
-            s = 0;
-            parity ^= 1;
-        }
-    }
-};
-
 __device__ __forceinline__ uint2 load8b(uint32_t at) {
     uint2 v;
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
@@ -192,7 +180,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::warps * 32, 1)
                 for (int g = 0; g < S::half / 16; ++g) {
                     uint32_t r[16];
                     tmem_ld16(at + (sum & 1) * NT + g * 16, r);
-                    tmem_wait_ld();
+                    tmem_wait_ld(r);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[g * 16 + i] += __uint_as_float(r[i]);
                 }
@@ -204,11 +192,14 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::warps * 32, 1)
             const int64_t row0 = int64_t(t / p.k_tiles) * NT + warp / 4 * S::half;
             const int64_t col = int64_t(t % p.k_tiles) * (2 * kCols) + half * kCols + warp % 4 * 32 + column_of(lane);
 #pragma unroll
-            for (int i = 0; i < S::half; ++i) {
-                if (split > 1)
-                    part_sums[(warp / 4 * S::half + i) * kCols + warp % 4 * 32 + column_of(lane)] = acc[i];
-                else if (row0 + i < out.rows && col < out.cols)
-                    out.put(row0 + i, col, acc[i]);
+            for (int i = 0; i < S::half; i += 16) {
+                if (split > 1) {
+#pragma unroll
+                    for (int j = i; j < i + 16; ++j)
+                        part_sums[(warp / 4 * S::half + j) * kCols + warp % 4 * 32 + column_of(lane)] = acc[j];
+                } else {
+                    out.put16(row0 + i, col, [&](int j) { return acc[i + j]; });
+                }
             }
         }
     } else if (warp < 12) {

@@ -57,6 +57,10 @@ cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint6
     return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, 2 * ld, 64, box_rows, true);
 }
 
+cudaError_t mx_scale_map(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_tiles) {
+    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, base, 128, tiles, 512, 128, box_tiles, false);
+}
+
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s) {
     const unsigned grid = static_cast<unsigned>(C.rows < 65536 ? C.rows : 65536);
     if (C.type == COSTA_MX_F32)

@@ -17,6 +17,8 @@ cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint
                         uint32_t box_rows, bool swizzle);
 cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t ld,
                         uint32_t box_rows);
+// Of tiles of scales (512 bytes), in boxes of `box_tiles`, not swizzled.
+cudaError_t mx_scale_map(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_tiles);
 // C = beta C (0 without reading C for beta == 0): products over nothing.
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s);
 // Waits that gave up, on the current device since the library was loaded.

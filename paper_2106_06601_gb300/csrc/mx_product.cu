@@ -5,7 +5,9 @@
 // and NT rows of A (its columns), so that a warp's lanes hold neighbouring
 // elements of a row of C and few rows of A need few columns.  Warp 4 brings
 // operands and scales into a ring of stages of 256 columns of k, one thread of
-// warp 5 issues the products, warps 0 to 3 write the tile out.
+// warp 5 issues the products, warps 0 to 3 write the tile out.  Tiles of 256
+// rows of A are taken by pairs of blocks, with 256 rows of B: each block then
+// brings half of A's rows, a third less for the L2 cache to deliver.
 #include <algorithm>
 
 #include "costa_internal.h"
@@ -22,7 +24,7 @@ constexpr int kRows = 128;   // rows of B in a tile
 __device__ unsigned g_failed;
 
 struct Params {
-    const uint8_t *a_scales, *b_scales;
+    const uint8_t *a_scales, *b_scales;  // not for pairs
     int64_t m;           // rows of A
     int steps;           // products of 64 elements over k
     int scale_tiles;     // tiles of scales over k
@@ -31,7 +33,9 @@ struct Params {
 
 // The columns of tensor memory and the stages of a tile of NT rows of A.
 template <int NT> struct Shape {
-    static constexpr int bands = NT > 128 ? 2 : 1;  // of 128 rows of A's scales
+    static constexpr bool pair = NT == 256;
+    static constexpr int blocks = pair ? 2 : 1, rows = blocks * kRows;  // of a tile
+    static constexpr int bands = NT > 128 ? 2 : 1;                      // of 128 rows of A's scales
     // Two sums of NT columns, so that one is written out while the next
     // builds.  Two of 256 would leave no room for the scales: they share
     // columns 208 .. 255, which the epilogue reads first (or, of the second
@@ -41,18 +45,21 @@ template <int NT> struct Shape {
     static constexpr int scale_cols = 8 + 8 * bands;  // of a stage: 2 tiles of B, 2 of each band of A
     static constexpr int used = scales + 2 * scale_cols;
     static constexpr int cols = used <= 64 ? 64 : used <= 128 ? 128 : used <= 256 ? 256 : 512;
-    static constexpr int b_bytes = kRows * 128, a_bytes = NT * 128, sf_bytes = 1024 * (1 + bands);
+    static constexpr int a_rows = NT / blocks;  // in a block
+    static constexpr int b_bytes = kRows * 128, a_bytes = a_rows * 128, sf_bytes = 1024 * (1 + bands);
     static constexpr int stage = (b_bytes + a_bytes + sf_bytes + 1023) / 1024 * 1024;
-    static constexpr int stages = NT == 256 ? 4 : NT == 128 ? 5 : 4;
+    static constexpr int stages = NT == 256 ? 6 : NT == 128 ? 5 : 4;
     static constexpr int smem = stages * stage + 1024;
-    static_assert(kRows * NT * 4 <= stages * stage, "a tile's partial sums fit the stages");
+    static_assert(smem <= 226 * 1024 && kRows * NT * 4 <= stages * stage, "a tile's partial sums fit the stages");
 };
 
 template <int NT, typename T>
-__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap a_map,
-                                                           const __grid_constant__ CUtensorMap b_map, const Params p,
-                                                           const Output<T> out, const int split) {
+__global__ void __launch_bounds__(kThreads, 1)
+    product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                   const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap b_scale_map,
+                   const Params p, const Output<T> out, const int split) {
     using S = Shape<NT>;
+    constexpr bool kPair = S::pair;
     constexpr int kLag = NT == 256 ? 1 : 2;  // the tile whose epilogue a tile waits for
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::stages + 4];
@@ -62,11 +69,12 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
     float *const part_sums = reinterpret_cast<float *>(raw + (ring - smem_addr(raw)));
     const uint32_t bar0 = smem_addr(bars);
-    auto full = [&](int s) { return bar0 + 8 * s; };
+    auto full = [&](int s) { return bar0 + 8 * s; };  // (a pair's first block's) operands have landed
     auto empty = [&](int s) { return bar0 + 8 * (S::stages + s); };
     auto sum_full = [&](int i) { return bar0 + 8 * (2 * S::stages + i); };
-    auto sum_empty = [&](int i) { return bar0 + 8 * (2 * S::stages + 2 + i); };
+    auto sum_empty = [&](int i) { return bar0 + 8 * (2 * S::stages + 2 + i); };  // (first block's)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int rank = static_cast<int>(cluster_rank()), half = kPair ? rank & 1 : 0;
 
     if (threadIdx.x == 0) {
         failed_word = 0;
@@ -76,76 +84,105 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(sum_full(i), 1);
-            bar_init(sum_empty(i), 4);
+            bar_init(sum_empty(i), 4 * S::blocks);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 5) tmem_alloc(&tmem_slot, S::cols);
+    if (warp == 5) {
+        if constexpr (kPair)
+            tmem_alloc_pair(&tmem_slot, S::cols);
+        else
+            tmem_alloc(&tmem_slot, S::cols);
+    }
     fence_before();
     __syncthreads();
+    if constexpr (kPair) cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
 
-    // This block's share of k, in stages; and its tiles.
+    // This block's share of k, in stages; and its tiles.  (Pairs do not split k.)
     const int stages_k = (p.steps + 3) / 4;
-    const int part = split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int part = kPair ? 0 : rank, per_tile = kPair ? 2 : split;
     const int k_first = static_cast<int>(int64_t(stages_k) * part / split);
     const int k_last = static_cast<int>(int64_t(stages_k) * (part + 1) / split);
-    const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / split, stride = gridDim.x / split;
+    const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / per_tile, stride = gridDim.x / per_tile;
 
     if (warp == 4) {
         if (elect_one()) {
-            int it = 0;
-            for (int t = first; t < tiles; t += stride) {
+            Ring<S::stages> at;
+            for (int t = first; t < tiles && !*failed; t += stride) {
                 const int nt = t / p.m_tiles, mt = t % p.m_tiles;
-                for (int k = k_first; k < k_last; ++k, ++it) {
-                    const int s = it % S::stages;
-                    if (it >= S::stages && !bar_wait(empty(s), (it / S::stages - 1) & 1, failed)) break;
-                    const uint32_t at = ring + s * S::stage, sf = at + S::b_bytes + S::a_bytes;
-                    const int sft = min(2, p.scale_tiles - 2 * k);  // tiles of scales of this stage
-                    // bands of A's scales that exist
-                    const int bands = S::bands == 2 && int64_t(mt) * NT + 128 < p.m ? 2 : 1;
-                    bar_expect(full(s), S::b_bytes + S::a_bytes + (1 + bands) * sft * 512);
-                    tma_load_2d(at, &b_map, k * 128, nt * kRows, full(s));
-                    tma_load_2d(at + S::b_bytes, &a_map, k * 128, mt * NT, full(s));
-                    bulk_load(sf, p.b_scales + (int64_t(nt) * p.scale_tiles + 2 * k) * 512, sft * 512, full(s));
-                    const int64_t band = int64_t(mt) * NT / 128;
-                    for (int b = 0; b < bands; ++b)
-                        bulk_load(sf + 1024 * (1 + b), p.a_scales + ((band + b) * p.scale_tiles + 2 * k) * 512, sft * 512,
-                                  full(s));
+                for (int k = k_first; k < k_last; ++k, at.next()) {
+                    if (!bar_wait(empty(at.s), at.parity ^ 1, failed)) break;
+                    const uint32_t to = ring + at.s * S::stage, sf = to + S::b_bytes + S::a_bytes, bar = full(at.s);
+                    if constexpr (kPair) {
+                        // tiles past the last over k, and bands past the last, bring what no product reads
+                        if (half == 0) bar_expect(bar, 2 * (S::b_bytes + S::a_bytes + S::sf_bytes));
+                        const int band = mt * 2, row = nt * 2 + half;
+                        tma_load_2d_at(to, &b_map, k * 128, row * kRows, bar, 0);
+                        tma_load_2d_at(to + S::b_bytes, &a_map, k * 128, mt * NT + half * S::a_rows, bar, 0);
+                        tma_load_2d_at(sf, &b_scale_map, 0, row * p.scale_tiles + 2 * k, bar, 0);
+                        for (int b = 0; b < 2; ++b)
+                            tma_load_2d_at(sf + 1024 * (1 + b), &a_scale_map, 0, (band + b) * p.scale_tiles + 2 * k, bar, 0);
+                    } else {
+                        const int sft = min(2, p.scale_tiles - 2 * k);  // tiles of scales of this stage
+                        bar_expect(bar, S::b_bytes + S::a_bytes + 2 * sft * 512);
+                        tma_load_2d(to, &b_map, k * 128, nt * kRows, bar);
+                        tma_load_2d(to + S::b_bytes, &a_map, k * 128, mt * NT, bar);
+                        bulk_load(sf, p.b_scales + (int64_t(nt) * p.scale_tiles + 2 * k) * 512, sft * 512, bar);
+                        bulk_load(sf + 1024, p.a_scales + (int64_t(mt) * p.scale_tiles + 2 * k) * 512, sft * 512, bar);
+                    }
                 }
-                if (*failed) break;
             }
         }
     } else if (warp == 5) {
-        if (elect_one()) {
-            int it = 0, done = 0;
+        if (half == 0 && elect_one()) {
+            auto commit = [&](uint32_t bar) {
+                if constexpr (kPair)
+                    mma_commit_pair(bar, 3);
+                else
+                    mma_commit(bar);
+            };
+            auto copy_scales = [&](uint32_t to, uint32_t from) {
+                if constexpr (kPair)
+                    scales_to_tmem_pair(to, scales_desc(from));
+                else
+                    scales_to_tmem(to, scales_desc(from));
+            };
+            Ring<S::stages> at;
+            int done = 0;
+            uint32_t turn = 0;
             for (int t = first; t < tiles && !*failed; t += stride, ++done) {
                 const uint32_t d = tmem + (done & 1 ? S::second : 0);
                 const int before = done - kLag;
                 if (before >= 0 && !bar_wait(sum_empty(before & 1), (before >> 1) & 1, failed)) break;
                 fence_after();
-                for (int k = k_first; k < k_last; ++k, ++it) {
-                    const int s = it % S::stages;
-                    if (!bar_wait(full(s), (it / S::stages) & 1, failed)) break;
+                for (int k = k_first; k < k_last; ++k, at.next()) {
+                    if (!bar_wait(full(at.s), at.parity, failed)) break;
                     fence_after();
-                    const uint32_t at = ring + s * S::stage, sf = at + S::b_bytes + S::a_bytes;
-                    const uint32_t sfd = tmem + S::scales + (it & 1) * S::scale_cols;
+                    const uint32_t from = ring + at.s * S::stage, sf = from + S::b_bytes + S::a_bytes;
+                    const uint32_t sfd = tmem + S::scales + turn * S::scale_cols;
+                    turn ^= 1;
                     const int steps = min(4, p.steps - 4 * k);
                     // columns of the scales: B's two tiles, then A's as (k tile, band)
                     for (int c = 0; 2 * c < steps; ++c) {
-                        scales_to_tmem(sfd + 4 * c, scales_desc(sf + 512 * c));
+                        copy_scales(sfd + 4 * c, sf + 512 * c);
                         for (int b = 0; b < S::bands; ++b)
-                            scales_to_tmem(sfd + 8 + 4 * (S::bands * c + b), scales_desc(sf + 1024 * (1 + b) + 512 * c));
+                            copy_scales(sfd + 8 + 4 * (S::bands * c + b), sf + 1024 * (1 + b) + 512 * c);
                     }
-                    const uint64_t da = operand_desc(at, 16, 1024), db = operand_desc(at + S::b_bytes, 16, 1024);
-                    for (int q = 0; q < steps; ++q)
-                        mma_e2m1(d, da + 2 * q, db + 2 * q, idesc_e2m1(NT, (q & 1) * 2), sfd + 4 * (q >> 1),
-                                 sfd + 8 + 4 * S::bands * (q >> 1), k > k_first || q > 0);
-                    mma_commit(empty(s));
+                    const uint64_t da = operand_desc(from, 16, 1024), db = operand_desc(from + S::b_bytes, 16, 1024);
+                    for (int q = 0; q < steps; ++q) {
+                        const uint32_t idesc = idesc_e2m1(S::rows, NT, (q & 1) * 2), sfa = sfd + 4 * (q >> 1),
+                                       sfb = sfd + 8 + 4 * S::bands * (q >> 1);
+                        if constexpr (kPair)
+                            mma_e2m1_pair(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > k_first || q > 0);
+                        else
+                            mma_e2m1(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > k_first || q > 0);
+                    }
+                    commit(empty(at.s));
                 }
                 if (*failed) break;
-                mma_commit(sum_full(done & 1));
+                commit(sum_full(done & 1));
             }
         }
     } else {
@@ -157,26 +194,58 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             constexpr int kChunks = NT / 16;
             // the shared columns first: chunks 13 .. 15 of the first sum, 0 .. 2 of the second
             const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0;
-            for (int j = 0; j < kChunks; ++j) {
-                tile_out16(out, d, (j + shift) % kChunks, int64_t(t % p.m_tiles) * NT, int64_t(t / p.m_tiles) * kRows,
-                           split > 1 ? part_sums : nullptr);
-                if (j == (kLag == 1 ? 2 : kChunks - 1)) {
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(sum_empty(done & 1));
+            const uint32_t lanes = d + (uint32_t(warp * 32) << 16);
+            const int64_t row0 = int64_t(t % p.m_tiles) * NT;
+            const int64_t col = int64_t(t / p.m_tiles) * S::rows + half * kRows + warp * 32 + lane;
+            auto load = [&](int j, uint32_t(&r)[16]) { tmem_ld16(lanes + (j + shift) % kChunks * 16, r); };
+            auto write = [&](int j, const uint32_t(&r)[16]) {
+                const int ch = (j + shift) % kChunks;
+                if (split > 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        part_sums[(ch * 16 + i) * kRows + warp * 32 + lane] = __uint_as_float(r[i]);
+                } else {
+                    out.put16(row0 + ch * 16, col, [&](int i) { return __uint_as_float(r[i]); });
+                }
+            };
+            // a chunk is loaded while the one before it is written
+            uint32_t r[2][16];
+            load(0, r[0]);
+#pragma unroll 1
+            for (int j = 0; j < kChunks; j += 2) {
+#pragma unroll
+                for (int h = 0; h < 2 && h < kChunks; ++h) {
+                    tmem_wait_ld(r[h]);
+                    if (j + h + 1 < kChunks) load(j + h + 1, r[1 - h]);
+                    if (j + h == (kLag == 1 ? 3 : kChunks - 1)) {  // (3: chunks 0 .. 2 have been read)
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (kPair)
+                                bar_arrive_at(sum_empty(done & 1), 0);
+                            else
+                                bar_arrive(sum_empty(done & 1));
+                        }
+                    }
+                    write(j + h, r[h]);
                 }
             }
         }
     }
+    __syncwarp();
 
     if (*failed) let_copies_land();
     if (split > 1)  // one tile to a cluster
         join_split(out, ring, 0, 1, part, split, int64_t(first % p.m_tiles) * NT, int64_t(first / p.m_tiles) * kRows, NT);
     fence_before();
     __syncthreads();
+    if constexpr (kPair) cluster_sync();  // neither block leaves while the other's products run
     if (warp == 5) {
         fence_after();
-        tmem_free(tmem, S::cols);
+        if constexpr (kPair)
+            tmem_free_pair(tmem, S::cols);
+        else
+            tmem_free(tmem, S::cols);
     }
     if (threadIdx.x == 0 && *failed) atomicAdd(&g_failed, 1u);
 }
@@ -186,9 +255,19 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
                    int sms, cudaStream_t s) {
     using S = Shape<NT>;
     const int64_t nb = mx_blocks(A.cols);
-    CUtensorMap a_map, b_map;
-    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, NT, true);
+    CUtensorMap a_map, b_map, a_scale_map, b_scale_map;
+    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, S::a_rows, true);
     if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows, true);
+    if constexpr (S::pair) {
+        const int64_t tiles_k = mx_scale_tiles(A.cols), a_tiles = mx_ceil(A.rows, 128) * tiles_k,
+                      b_tiles = mx_ceil(B.rows, 128) * tiles_k;
+        if (a_tiles > INT32_MAX / 2 || b_tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+        if (e == cudaSuccess) e = mx_scale_map(&a_scale_map, A.scales, a_tiles, 2);
+        if (e == cudaSuccess) e = mx_scale_map(&b_scale_map, B.scales, b_tiles, 2);
+    } else {
+        a_scale_map = a_map;
+        b_scale_map = b_map;
+    }
     if (e != cudaSuccess) return e;
     Params p;
     p.a_scales = static_cast<const uint8_t *>(A.scales);
@@ -196,27 +275,28 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     p.m = C.rows;
     p.steps = static_cast<int>(mx_ceil(nb, 2));
     p.scale_tiles = static_cast<int>(mx_scale_tiles(A.cols));
-    p.n_tiles = static_cast<int>(mx_ceil(C.cols, kRows));
+    p.n_tiles = static_cast<int>(mx_ceil(C.cols, S::rows));
     p.m_tiles = static_cast<int>(mx_ceil(C.rows, NT));
     const Output<T> out{static_cast<T *>(C.ptr), C.ld, C.rows, C.cols, alpha, beta};
     const int64_t tiles = int64_t(p.n_tiles) * p.m_tiles;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     const int stages_k = (p.steps + 3) / 4;
     int split = 1;
-    while (split < 8 && tiles * split * 2 <= 2 * sms && stages_k >= 4 * split) split *= 2;
+    while (!S::pair && split < 8 && tiles * split * 2 <= 2 * sms && stages_k >= 4 * split) split *= 2;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(split > 1 ? tiles * split : std::min<int64_t>(tiles, sms)));
+    cfg.gridDim = dim3(static_cast<unsigned>(
+        S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks))));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = S::smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {static_cast<unsigned>(split), 1, 1};
+    at[0].val.clusterDim = {static_cast<unsigned>(S::blocks * split), 1, 1};
     cfg.attrs = at;
     cfg.numAttrs = 1;
     e = cudaFuncSetAttribute(product_kernel<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
     if (e != cudaSuccess) return e;
-    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, p, out, split);
+    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, a_scale_map, b_scale_map, p, out, split);
     if (e == cudaSuccess) count_launch();
     return e;
 }
@@ -227,7 +307,7 @@ cudaError_t by_rows(const costa_mx_matrix &A, const costa_mx_matrix &B, float al
     if (C.rows <= 16) return launch<16, T>(A, B, alpha, beta, C, sms, s);
     if (C.rows <= 32) return launch<32, T>(A, B, alpha, beta, C, sms, s);
     if (C.rows <= 64) return launch<64, T>(A, B, alpha, beta, C, sms, s);
-    if (C.rows <= 128 || mx_ceil(C.rows, 256) * mx_ceil(C.cols, kRows) < sms)
+    if (C.rows <= 128 || mx_ceil(C.rows, 256) * mx_ceil(C.cols, 256) < sms / 2)
         return launch<128, T>(A, B, alpha, beta, C, sms, s);
     return launch<256, T>(A, B, alpha, beta, C, sms, s);
 }

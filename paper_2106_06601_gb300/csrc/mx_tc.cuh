@@ -70,6 +70,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return false;
 }
 
+// A place in a ring of N stages and the parity of its barriers' current phase.
+template <int N> struct Ring {
+    int s = 0;
+    uint32_t parity = 0;
+    __device__ void next() {
+        if (++s == N) {
+            s = 0;
+            parity ^= 1;
+        }
+    }
+};
+
 // Some milliseconds, far longer than any copy in flight takes.
 __device__ __forceinline__ void let_copies_land() {
     const long long start = clock64();
@@ -140,7 +152,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads so far; r, of one of them, is not used before.
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
 
 // ---- descriptors ----
 
@@ -168,9 +185,22 @@ __device__ __forceinline__ void mma_e2m1(uint32_t d, uint64_t a, uint64_t b, uin
         "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(uint32_t(accumulate))
         : "memory");
 }
-// E2M1 x E2M1, scales of exponents only, 128 rows; which half of the scales' 4 bytes: 0 or 2.
-__device__ __forceinline__ constexpr uint32_t idesc_e2m1(int n, int half) {
-    return uint32_t(half) << 4 | 1u << 7 | 1u << 10 | uint32_t(n >> 3) << 17 | 1u << 23 | uint32_t(128 >> 4) << 24 |
+// The same for D[256 x n] by a pair of blocks: each holds 128 rows of A (with
+// their scales) and of D, half of B's rows, and the scales of all of them.
+__device__ __forceinline__ void scales_to_tmem_pair(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_e2m1_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa,
+                                              uint32_t sfb, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(uint32_t(accumulate))
+        : "memory");
+}
+// E2M1 x E2M1, scales of exponents only, m x n; which half of the scales' 4 bytes: 0 or 2.
+__device__ __forceinline__ constexpr uint32_t idesc_e2m1(int m, int n, int half) {
+    return uint32_t(half) << 4 | 1u << 7 | 1u << 10 | uint32_t(n >> 3) << 17 | 1u << 23 | uint32_t(m >> 4) << 24 |
            uint32_t(half) << 29;
 }
 
@@ -228,30 +258,24 @@ template <typename T> struct Output {
         if (beta != 0.0f) v += beta * to_float(*at);
         *at = from_float<T>(v);
     }
-};
-
-// Columns 16 ch .. 16 ch + 15 of a tile's sums: rows of the output from row0
-// (the tile's first), each warp's lanes at neighbouring columns from col0.
-// With `part` not null they are kept there instead, 128 to a row.
-template <typename T>
-__device__ __forceinline__ void tile_out16(const Output<T> &out, uint32_t tmem, int ch, int64_t row0, int64_t col0,
-                                           float *part) {
-    const int warp = threadIdx.x / 32 % 4, lane = threadIdx.x % 32;
-    const int64_t row = row0 + ch * 16, col = col0 + warp * 32 + lane;
-    if (row >= out.rows) return;
-    uint32_t r[16];
-    tmem_ld16(tmem + (uint32_t(warp * 32) << 16) + ch * 16, r);
-    tmem_wait_ld();
-    if (part) {
+    // The sums sum(0) .. sum(15) of 16 rows of a column.
+    template <typename F> __device__ void put16(int64_t row, int64_t col, F sum) const {
+        if (col >= cols || row >= rows) return;
+        T *at = p + row * ld + col;
+        if (beta == 0.0f && row + 16 <= rows) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) part[(ch * 16 + i) * 128 + warp * 32 + lane] = __uint_as_float(r[i]);
-    } else if (col < out.cols) {
-        const int rows = static_cast<int>(min(int64_t(16), out.rows - row));
+            for (int i = 0; i < 16; ++i, at += ld) *at = from_float<T>(alpha * sum(i));
+            return;
+        }
+        const int n = static_cast<int>(min(int64_t(16), rows - row));
+        float old[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i < rows) out.put(row + i, col, __uint_as_float(r[i]));
+        for (int i = 0; i < 16; ++i) old[i] = beta != 0.0f && i < n ? beta * to_float(at[i * ld]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i, at += ld)
+            if (i < n) *at = from_float<T>(alpha * sum(i) + old[i]);
     }
-}
+};
 
 // Joins the partial sums of `split` blocks of a cluster (at shared address
 // `part` of the blocks first, first + step, ...), in that order; each of them,
