@@ -26,23 +26,28 @@ template <int FMT> __device__ __forceinline__ int scale_byte(int e) {
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Two E2M1 codes, a in the low half.  The conversion rounds to nearest even and saturates at 6.
-__device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
+// E2M1 codes of 8 numbers x(0) .. x(7), the first in the low bits; the
+// conversion rounds to nearest even and saturates at 6.
+template <typename X> __device__ __forceinline__ uint32_t e2m1_of8(const X &x) {
     uint32_t r;
-    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\tmov.b32 %0, {t, 0, 0, 0};\n\t}" : "=r"(r) : "f"(a), "f"(b));
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(x(0)), "f"(x(1)), "f"(x(2)), "f"(x(3)), "f"(x(4)), "f"(x(5)), "f"(x(6)), "f"(x(7)));
     return r;
 }
 
-// Codes of 8 elements x(0) .. x(7), for scale byte s; zero codes for 255.  What
-// takes an element to its code's range is a normal power of two (two of them
-// for I8 below 2^-121, where 2^(6 - E) is beyond a float), so the products are
-// exact unless they are subnormal, far below half of the least code.
-template <typename X> __device__ __forceinline__ uint32_t e2m1_of8(const X &x, int s) {
-    if (s == 255) return 0;
-    const float f = pow2(254 - s);  // s <= 252
-    return e2m1x2(x(0) * f, x(1) * f) | e2m1x2(x(2) * f, x(3) * f) << 8 | e2m1x2(x(4) * f, x(5) * f) << 16 |
-           e2m1x2(x(6) * f, x(7) * f) << 24;
-}
+// What takes a block's elements to its codes' range: a normal power of two, so
+// the products are exact unless they are subnormal, far below half of the least
+// code (as are bf16 products); 0 for NaN blocks, whose codes are then cleared.
+// I8 below 2^-121, where 2^(6 - E) is beyond a float, takes 2^6 apart.
+__device__ __forceinline__ float e2m1_factor(int s) { return s == 255 ? 0.0f : pow2(254 - s); }  // s <= 252
+__device__ __forceinline__ __nv_bfloat162 halves(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); }
+__device__ __forceinline__ uint32_t word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // Added to 1.5 2^23 a number below 2^22 is rounded to an integer, to nearest
 // even, in the low bits; they are clamped in pairs of 16 bits.
@@ -71,16 +76,26 @@ __device__ __forceinline__ float i8_unit(int s) {
     return __uint_as_float(bits);
 }
 
-// Values of 4 codes of E2M1 (the low 16 bits) and of I8.  The three low bits of
-// an E2M1 code are the exponent and fraction of a float 2^126 times smaller (0.5
-// a subnormal one); an I8 code q is taken as the float 2^23 + 128 + q.
-__device__ __forceinline__ void e2m1_to4(uint32_t codes, float unit, float (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t top = codes << (28 - 4 * i);  // the code in the top four bits
-        v[i] = __uint_as_float((top & 0x80000000u) | (top >> 6 & 0x01c00000u)) * 0x1p126f * unit;
-    }
+// Values of 4 codes of E2M1 (the low 16 bits) as bf16 pairs.  A byte permutation
+// looks up the high and the low bytes of 0, 0.5, 1, 1.5, 2, 3, 4, 6 by three bits
+// of each code; one with the whole code gives 0x40, or 0 (the selected byte's
+// sign throughout) where the sign is set.
+__device__ __forceinline__ void e2m1_to4(uint32_t codes, __nv_bfloat162 unit, uint32_t (&v)[2]) {
+    const uint32_t which = codes & 0x7777u;
+    uint32_t high = __byte_perm(0x3f3f3f00u, 0x40404040u, which);
+    const uint32_t low = __byte_perm(0xc0800000u, 0xc0804000u, which);
+    uint32_t plus;
+    asm("prmt.b32 %0, %1, %1, %2;" : "=r"(plus) : "r"(0x40404040u), "r"(codes));
+    high |= ~(plus << 1) & 0x80808080u;
+    v[0] = word(__hmul2(halves(__byte_perm(low, high, 0x5140)), unit));
+    v[1] = word(__hmul2(halves(__byte_perm(low, high, 0x7362)), unit));
 }
+// The unit of E2M1 codes with scale byte s, 2^(s - 127), as a bf16 pair.
+__device__ __forceinline__ __nv_bfloat162 e2m1_unit(int s) {
+    return halves((s == 0 ? 0x0040u : s == 255 ? 0x7fffu : uint32_t(s) << 7) * 0x10001u);
+}
+
+// Values of 4 codes of I8: a code q is taken as the float 2^23 + 128 + q.
 __device__ __forceinline__ void i8_to4(uint32_t codes, float unit, float (&v)[4]) {
     const uint32_t w = codes ^ 0x80808080u;
 #pragma unroll

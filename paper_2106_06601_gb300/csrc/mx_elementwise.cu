@@ -72,6 +72,15 @@ template <> struct Sixteen<float> {
         for (int i = 0; i < 16; ++i) a = max(a, w[i] & 0x7fffffffu);
         return a >> 23;
     }
+    __device__ uint2 e2m1(float f) const {
+        return make_uint2(e2m1_of8([&](int i) { return (*this)(i) * f; }), e2m1_of8([&](int i) { return (*this)(i + 8) * f; }));
+    }
+    __device__ void set_pairs(int i, const uint32_t (&v)[2]) {
+        w[i] = v[0] << 16;
+        w[i + 1] = v[0] & 0xffff0000u;
+        w[i + 2] = v[1] << 16;
+        w[i + 3] = v[1] & 0xffff0000u;
+    }
 };
 template <> struct Sixteen<__nv_bfloat16> {
     uint32_t w[8];
@@ -87,6 +96,18 @@ template <> struct Sixteen<__nv_bfloat16> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a = __vmaxu2(a, w[i] & 0x7fff7fffu);
         return max(a & 0xffffu, a >> 16) >> 7;
+    }
+    __device__ uint2 e2m1(float f) const {
+        const __nv_bfloat162 ff = __float2bfloat162_rn(f);
+        uint32_t t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = word(__hmul2(halves(w[i]), ff));
+        auto at = [&](int i) { return i % 2 ? high_of(t[i / 2]) : low_of(t[i / 2]); };
+        return make_uint2(e2m1_of8(at), e2m1_of8([&](int i) { return at(i + 8); }));
+    }
+    __device__ void set_pairs(int i, const uint32_t (&v)[2]) {
+        w[i / 2] = v[0];
+        w[i / 2 + 1] = v[1];
     }
 };
 
@@ -105,15 +126,43 @@ __device__ __forceinline__ void store32(void *p, const uint32_t *w) {
 // The elements of a warp's 32 groups where rows are not aligned or end inside a
 // group: the lanes take a block's 32 elements together, through 2 KB of shared
 // memory of the warp.  Lane 2 i holds block i's place and how many of its
-// elements exist.
+// elements exist; in most warps all blocks follow each other in a row.
 struct Blocks {
-    int64_t place;
-    int count;
+    int64_t place, first;
+    int count, left;
+    bool run;
     __device__ Blocks(int64_t row, int64_t col, int64_t cols, int64_t ld)
-        : place(row * ld + col), count(static_cast<int>(max(int64_t(0), min(int64_t(32), cols - col)))) {}
-    __device__ int64_t place_of(int i) const { return __shfl_sync(~0u, place, 2 * i); }
-    __device__ int count_of(int i) const { return __shfl_sync(~0u, count, 2 * i); }
+        : place(row * ld + col), count(static_cast<int>(max(int64_t(0), min(int64_t(32), cols - col)))) {
+        const int lane = threadIdx.x % 32;
+        first = __shfl_sync(~0u, place, 0);
+        run = __all_sync(~0u, place == first + 16 * lane || count == 0);
+        // elements from the first on: whole blocks, then one that may end, then none
+        left = __reduce_add_sync(~0u, lane % 2 ? 0 : count);
+    }
+    // f(i, place) for this lane's element of blocks from .. from + N - 1, where it exists.
+    template <int N, typename F> __device__ void each(int from, F f) const {
+        const int lane = threadIdx.x % 32;
+        if (run) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (32 * (from + i) + lane < left) f(i, first + lane + 32 * (from + i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t p = __shfl_sync(~0u, place, 2 * (from + i));
+                if (lane < __shfl_sync(~0u, count, 2 * (from + i))) f(i, p + lane);
+            }
+        }
+    }
 };
+
+// Where a lane's q-th four elements lie in the warp's shared memory (the four
+// are exchanged so that 8 lanes fill all banks), and where element `lane` of
+// block i does.
+__device__ __forceinline__ int four_at(int lane, int q) { return 16 * lane + 4 * (q ^ (lane >> 1 & 3)); }
+__device__ __forceinline__ int element_at(int i, int lane) {
+    return 32 * i + (lane & 16) + 4 * ((lane >> 2 & 3) ^ (i & 3)) + (lane & 3);
+}
 
 // This thread's 16 elements, 0 past the row's end.  Whole warps call this.
 template <typename T>
@@ -142,19 +191,15 @@ __device__ __forceinline__ void get(const Dense<const T> &X, int64_t row, int64_
     __syncwarp();
 #pragma unroll
     for (int h = 0; h < 16; h += 8) {
-        float v[8];
+        float v[8] = {};
+        b.each<8>(h, [&](int i, int64_t at) { v[i] = to_float(X.p[at]); });
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t place = b.place_of(h + i);
-            v[i] = lane < b.count_of(h + i) ? to_float(X.p[place + lane]) : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) stage[32 * (h + i) + lane] = v[i];
+        for (int i = 0; i < 8; ++i) stage[element_at(h + i, lane)] = v[i];
     }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-        const float4 v = reinterpret_cast<const float4 *>(stage)[4 * lane + i / 4];
+        const float4 v = *reinterpret_cast<const float4 *>(stage + four_at(lane, i / 4));
         x.set(i, v.x);
         x.set(i + 1, v.y);
         x.set(i + 2, v.z);
@@ -183,13 +228,9 @@ __device__ __forceinline__ void put(const Dense<T> &Y, int64_t row, int64_t col,
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 16; i += 4)
-        reinterpret_cast<float4 *>(stage)[4 * lane + i / 4] = make_float4(x(i), x(i + 1), x(i + 2), x(i + 3));
+        *reinterpret_cast<float4 *>(stage + four_at(lane, i / 4)) = make_float4(x(i), x(i + 1), x(i + 2), x(i + 3));
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t place = b.place_of(i);
-        if (lane < b.count_of(i)) Y.p[place + lane] = from_float<T>(stage[32 * i + lane]);
-    }
+    b.each<16>(0, [&](int i, int64_t at) { Y.p[at] = from_float<T>(stage[element_at(i, lane)]); });
 }
 
 #define COSTA_MX_STAGE                                        \
@@ -215,11 +256,13 @@ __device__ __forceinline__ int put_codes(const Codes &q, bool in, int64_t row, i
     const int e = x.exponent();
     const int s = scale_byte<FMT>(max(e, __shfl_xor_sync(~0u, e, 1)));
     if (in && col < ((cols + 31) & ~int64_t(31))) {
-        auto low = [&](int i) { return x(i); };
-        auto high = [&](int i) { return x(i + 8); };
         if constexpr (FMT == COSTA_MX_E2M1) {
-            *reinterpret_cast<uint2 *>(q.codes + row * q.ld + col / 2) = make_uint2(e2m1_of8(low, s), e2m1_of8(high, s));
+            uint2 w = x.e2m1(e2m1_factor(s));
+            if (s == 255) w = make_uint2(0, 0);
+            *reinterpret_cast<uint2 *>(q.codes + row * q.ld + col / 2) = w;
         } else {
+            auto low = [&](int i) { return x(i); };
+            auto high = [&](int i) { return x(i + 8); };
             const uint2 a = i8_of8(low, s), b = i8_of8(high, s);
             *reinterpret_cast<uint4 *>(q.codes + row * q.ld + col) = make_uint4(a.x, a.y, b.x, b.y);
         }
@@ -239,31 +282,19 @@ __device__ __forceinline__ void put16(const Codes &q, bool in, int64_t row, int6
         q.scales[row * q.unit + (col >> 5)] = static_cast<uint8_t>(s);
 }
 
-// 16 codes and what they are multiples of.
-template <int FMT> struct Coded {
-    uint32_t w[FMT == COSTA_MX_E2M1 ? 2 : 4];
+// 16 codes of I8 and what they are multiples of.
+struct Coded {
+    uint32_t w[4];
     float unit;
     __device__ void load(const Codes &q, int64_t row, int64_t col) {
-        if constexpr (FMT == COSTA_MX_E2M1) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(q.codes + row * q.ld + col / 2);
-            w[0] = v.x;
-            w[1] = v.y;
-            unit = pow2(q.scales[scale_at(row, col >> 5, q.unit)]);
-        } else {
-            const uint4 v = *reinterpret_cast<const uint4 *>(q.codes + row * q.ld + col);
-            w[0] = v.x;
-            w[1] = v.y;
-            w[2] = v.z;
-            w[3] = v.w;
-            unit = i8_unit(q.scales[row * q.unit + (col >> 5)]);
-        }
+        const uint4 v = *reinterpret_cast<const uint4 *>(q.codes + row * q.ld + col);
+        w[0] = v.x;
+        w[1] = v.y;
+        w[2] = v.z;
+        w[3] = v.w;
+        unit = i8_unit(q.scales[row * q.unit + (col >> 5)]);
     }
-    __device__ void four(int i, float (&v)[4]) const {  // values of codes 4 i .. 4 i + 3
-        if constexpr (FMT == COSTA_MX_E2M1)
-            e2m1_to4(w[i / 2] >> (i % 2 * 16), unit, v);
-        else
-            i8_to4(w[i], unit, v);
-    }
+    __device__ void four(int i, float (&v)[4]) const { i8_to4(w[i], unit, v); }  // values of codes 4 i .. 4 i + 3
 };
 
 // Groups of a row of codes: whole blocks, and for E2M1 whole scale tiles.
@@ -286,15 +317,31 @@ template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> Y, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
-    Coded<FMT> q;
-    if (gr.at(cols, row, col)) q.load(Q, row, col);
+    const bool in = gr.at(cols, row, col);
     Sixteen<T> y;
+    if constexpr (FMT == COSTA_MX_E2M1) {
+        uint2 w{};
+        __nv_bfloat162 unit = e2m1_unit(0);
+        if (in) {
+            w = *reinterpret_cast<const uint2 *>(Q.codes + row * Q.ld + col / 2);
+            unit = e2m1_unit(Q.scales[scale_at(row, col >> 5, Q.unit)]);
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float v[4];
-        q.four(i, v);
+        for (int i = 0; i < 4; ++i) {
+            uint32_t v[2];
+            e2m1_to4((i < 2 ? w.x : w.y) >> (i % 2 * 16), unit, v);
+            y.set_pairs(4 * i, v);
+        }
+    } else {
+        Coded q{};
+        if (in) q.load(Q, row, col);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y.set(4 * i + j, v[j]);
+        for (int i = 0; i < 4; ++i) {
+            float v[4];
+            q.four(i, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y.set(4 * i + j, v[j]);
+        }
     }
     put(Y, row, col, cols, stage, y);
 }
@@ -309,8 +356,28 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> 
 // then read again, from the cache, 8 lanes to a row.
 constexpr int kTile = 128;
 
+// The codes of a block of 32 elements x(0) .. x(31) with scale byte s (E2M1: taken
+// to the codes' range already), to shared memory.
+template <int FMT, typename F> __device__ __forceinline__ void block_codes(uint8_t *to, int s, F x) {
+    constexpr int kWords = FMT == COSTA_MX_E2M1 ? 4 : 8;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        auto y = [&](int i) { return x(8 * k + i); };
+        if constexpr (FMT == COSTA_MX_E2M1) {
+            w[k] = s == 255 ? 0 : e2m1_of8(y);
+        } else {
+            const uint2 u = i8_of8(y, s);
+            w[2 * k] = u.x;
+            w[2 * k + 1] = u.y;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kWords; k += 4) reinterpret_cast<uint4 *>(to)[k / 4] = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+}
+
 template <typename T, int FMT, bool BOTH>
-__global__ void __launch_bounds__(kThreads, 2) quantize_t_kernel(Dense<const T> X, bool pairs, int64_t rows, int64_t cols,
+__global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> X, bool pairs, int64_t rows, int64_t cols,
                                                                  Codes QN, Codes QT, unsigned col_tiles) {
     constexpr int kBlockBytes = FMT == COSTA_MX_E2M1 ? 16 : 32, kPitch = 4 * kBlockBytes + 16;
     __shared__ __align__(16) uint8_t codes[kTile * kPitch];
@@ -318,58 +385,53 @@ __global__ void __launch_bounds__(kThreads, 2) quantize_t_kernel(Dense<const T> 
     COSTA_MX_STAGE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, block = warp % 4, left = warp / 4 * 64;
     const int64_t r0 = int64_t(blockIdx.x / col_tiles) * kTile, c0 = int64_t(blockIdx.x % col_tiles) * kTile;
-    float x[2][32];
+    const int in_rows = static_cast<int>(max(int64_t(0), min(int64_t(32), rows - r0 - 32 * block)));
     if (sizeof(T) == 2 && pairs) {
         const int64_t c = c0 + left + 2 * lane;
         const T *p = X.p + (r0 + 32 * block) * X.ld + c;
-        uint32_t v[32];
+        const int in_cols = static_cast<int>(max(int64_t(0), min(int64_t(2), cols - c)));
+        uint32_t v[32], a = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const bool in = r0 + 32 * block + i < rows;
+        for (int i = 0; i < 32; ++i, p += X.ld) {
             v[i] = 0;
-            if (in && c + 1 < cols)
-                v[i] = *reinterpret_cast<const uint32_t *>(p + i * X.ld);
-            else if (in && c < cols)
-                v[i] = *reinterpret_cast<const uint16_t *>(p + i * X.ld);
+            if (i < in_rows && in_cols == 2)
+                v[i] = *reinterpret_cast<const uint32_t *>(p);
+            else if (i < in_rows && in_cols == 1)
+                v[i] = *reinterpret_cast<const uint16_t *>(p);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            x[0][i] = __uint_as_float(v[i] << 16);
-            x[1][i] = __uint_as_float(v[i] & 0xffff0000u);
+        for (int i = 0; i < 32; ++i) a = __vmaxu2(a, v[i] & 0x7fff7fffu);
+        const int sc2[2] = {scale_byte<FMT>((a & 0xffffu) >> 7), scale_byte<FMT>(a >> 23)};
+        if constexpr (FMT == COSTA_MX_E2M1) {
+            const __nv_bfloat162 f = __floats2bfloat162_rn(e2m1_factor(sc2[0]), e2m1_factor(sc2[1]));
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = word(__hmul2(halves(v[i]), f));
         }
-    } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t c = c0 + left + lane + 32 * h;
-            const T *p = X.p + (r0 + 32 * block) * X.ld + c;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[h][i] = c < cols && r0 + 32 * block + i < rows ? to_float(p[i * X.ld]) : 0.0f;
+            const int col = left + 2 * lane + h;
+            sc[0][col][block] = static_cast<uint8_t>(sc2[h]);
+            block_codes<FMT>(codes + col * kPitch + block * kBlockBytes, sc2[h],
+                             [&](int i) { return h ? high_of(v[i]) : low_of(v[i]); });
         }
-    }
+    } else {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int col = left + lane + 32 * h;
+            const T *p = X.p + (r0 + 32 * block) * X.ld + c0 + col;
+            const int in = c0 + col < cols ? in_rows : 0;
+            float x[32];
+            uint32_t a = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int col = left + (sizeof(T) == 2 && pairs ? 2 * lane + h : lane + 32 * h);
-        uint32_t a = 0;
+            for (int i = 0; i < 32; ++i, p += X.ld) x[i] = i < in ? to_float(*p) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) a = max(a, magnitude(x[h][i]));
-        const int s = scale_byte<FMT>(a >> 23);
-        uint8_t *to = codes + col * kPitch + block * kBlockBytes;
-        sc[0][col][block] = static_cast<uint8_t>(s);
-        uint32_t w[kBlockBytes / 4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            auto y = [&](int i) { return x[h][8 * k + i]; };
-            if constexpr (FMT == COSTA_MX_E2M1) {
-                w[k] = e2m1_of8(y, s);
-            } else {
-                const uint2 u = i8_of8(y, s);
-                w[2 * k] = u.x;
-                w[2 * k + 1] = u.y;
-            }
+            for (int i = 0; i < 32; ++i) a = max(a, magnitude(x[i]));
+            const int s = scale_byte<FMT>(a >> 23);
+            sc[0][col][block] = static_cast<uint8_t>(s);
+            const float f = FMT == COSTA_MX_E2M1 ? e2m1_factor(s) : 1.0f;
+            block_codes<FMT>(codes + col * kPitch + block * kBlockBytes, s,
+                             [&](int i) { return FMT == COSTA_MX_E2M1 ? x[i] * f : x[i]; });
         }
-#pragma unroll
-        for (int k = 0; k < kBlockBytes / 16; ++k)
-            reinterpret_cast<uint4 *>(to)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
     }
     __syncthreads();
     const int64_t nb = (rows + 31) >> 5, b0 = r0 >> 5;  // blocks of a row of QT; the first of these
@@ -427,10 +489,27 @@ __device__ __forceinline__ float sigmoid(float x) {
     return r;
 }
 
+// The normal distribution's cdf at x, and e^(-x^2 / 2): Abramowitz and Stegun's
+// 7.1.26, five terms in t = 1 / (1 + p |x| / sqrt(2)), within 0.75e-7.
+__device__ __forceinline__ float normal_cdf(float x, float &e) {
+    float t;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(fabsf(x), 0.3275911f * 0.7071067811865476f, 1.0f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * x * (-0.5f * 1.4426950408889634f)));
+    float s = fmaf(t, 1.061405429f, -1.453152027f);
+    s = fmaf(t, s, 1.421413741f);
+    s = fmaf(t, s, -0.284496736f);
+    s = fmaf(t, s, 0.254829592f);
+    const float tail = 0.5f * t * s * e;
+    return x < 0.0f ? tail : 1.0f - tail;
+}
+
 // act(x) and act'(x).
 template <int ACT> __device__ __forceinline__ float act(float x) {
     if constexpr (ACT == COSTA_MX_SILU) return x * sigmoid(x);
-    if constexpr (ACT == COSTA_MX_GELU) return x * (0.5f + 0.5f * erff(x * 0.7071067811865476f));
+    if constexpr (ACT == COSTA_MX_GELU) {
+        float e;
+        return x * normal_cdf(x, e);
+    }
     return x > 0.0f || x != x ? x : 0.0f;
 }
 template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, float &slope) {
@@ -439,9 +518,10 @@ template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, f
         y = x * s;
         slope = s * (1.0f + x * (1.0f - s));
     } else if constexpr (ACT == COSTA_MX_GELU) {
-        const float c = 0.5f + 0.5f * erff(x * 0.7071067811865476f);
+        float e;
+        const float c = normal_cdf(x, e);
         y = x * c;
-        slope = c + x * __expf(-0.5f * x * x) * 0.3989422804014327f;
+        slope = fmaf(x * e, 0.3989422804014327f, c);
     } else {
         y = act<ACT>(x);
         slope = x != x ? x : x > 0.0f ? 1.0f : 0.0f;
@@ -449,7 +529,7 @@ template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, f
 }
 
 template <typename T, int ACT, bool GATED>
-__global__ void __launch_bounds__(kThreads) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
+__global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
                                                                Codes QG, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
@@ -465,13 +545,13 @@ __global__ void __launch_bounds__(kThreads) act_forward_kernel(Dense<const T> X,
 }
 
 template <typename T, int ACT, bool GATED>
-__global__ void __launch_bounds__(kThreads) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
                                                                 Dense<T> dG, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
     const bool in = gr.at(cols, row, col);
     Sixteen<T> d, dx, dg;
-    Coded<COSTA_MX_I8> x, g;
+    Coded x{}, g{};
     if (in) {
         x.load(QX, row, col);
         if constexpr (GATED) g.load(QG, row, col);

@@ -18,7 +18,7 @@ namespace mx {
 namespace {
 
 constexpr int kThreads = 192;
-constexpr int kRows = 128;   // rows of B in a tile
+constexpr int kRows = 128;  // rows of B in a block's tile
 // A stage holds 256 elements of k: 128 bytes of a row, 2 tiles of scales.
 
 __device__ unsigned g_failed;
@@ -190,13 +190,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int t = first; t < tiles; t += stride, ++done) {
             if (!__all_sync(~0u, bar_wait(sum_full(done & 1), (done >> 1) & 1, failed))) break;
             fence_after();
+            const int nt = t / p.m_tiles, mt = t % p.m_tiles;
             const uint32_t d = tmem + (done & 1 ? S::second : 0);
             constexpr int kChunks = NT / 16;
             // the shared columns first: chunks 13 .. 15 of the first sum, 0 .. 2 of the second
             const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0;
             const uint32_t lanes = d + (uint32_t(warp * 32) << 16);
-            const int64_t row0 = int64_t(t % p.m_tiles) * NT;
-            const int64_t col = int64_t(t / p.m_tiles) * S::rows + half * kRows + warp * 32 + lane;
+            const int64_t row0 = int64_t(mt) * NT;
+            const int64_t col = int64_t(nt) * S::rows + half * kRows + warp * 32 + lane;
             auto load = [&](int j, uint32_t(&r)[16]) { tmem_ld16(lanes + (j + shift) % kChunks * 16, r); };
             auto write = [&](int j, const uint32_t(&r)[16]) {
                 const int ch = (j + shift) % kChunks;
@@ -208,25 +209,40 @@ __global__ void __launch_bounds__(kThreads, 1)
                     out.put16(row0 + ch * 16, col, [&](int i) { return __uint_as_float(r[i]); });
                 }
             };
+            auto drained = [&] {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (kPair)
+                        bar_arrive_at(sum_empty(done & 1), 0);
+                    else
+                        bar_arrive(sum_empty(done & 1));
+                }
+            };
+            constexpr int kFirst = kLag == 1 ? 3 : 0;  // the shared columns, all read before any is written
+            if constexpr (kFirst > 0) {
+                uint32_t r[kFirst][16];
+#pragma unroll
+                for (int j = 0; j < kFirst; ++j) load(j, r[j]);
+#pragma unroll
+                for (int j = 0; j < kFirst; ++j) tmem_wait_ld(r[j]);
+                drained();
+#pragma unroll
+                for (int j = 0; j < kFirst; ++j) write(j, r[j]);
+            }
             // a chunk is loaded while the one before it is written
             uint32_t r[2][16];
-            load(0, r[0]);
+            load(kFirst, r[0]);
 #pragma unroll 1
-            for (int j = 0; j < kChunks; j += 2) {
+            for (int j = kFirst; j < kChunks; j += 2) {
 #pragma unroll
-                for (int h = 0; h < 2 && h < kChunks; ++h) {
+                for (int h = 0; h < 2; ++h) {
+                    if (j + h >= kChunks) break;
                     tmem_wait_ld(r[h]);
-                    if (j + h + 1 < kChunks) load(j + h + 1, r[1 - h]);
-                    if (j + h == (kLag == 1 ? 3 : kChunks - 1)) {  // (3: chunks 0 .. 2 have been read)
-                        fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if constexpr (kPair)
-                                bar_arrive_at(sum_empty(done & 1), 0);
-                            else
-                                bar_arrive(sum_empty(done & 1));
-                        }
-                    }
+                    if (j + h + 1 < kChunks)
+                        load(j + h + 1, r[1 - h]);
+                    else if (kFirst == 0)
+                        drained();
                     write(j + h, r[h]);
                 }
             }
