@@ -10,6 +10,11 @@
 namespace costa {
 namespace mx {
 
+// The first call of every kernel: from here on the next kernel's blocks may start.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Before anything in global memory is read or written: what the kernels before this one wrote is there.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // 2^(biased - 127) for biased in 0 .. 254; NaN for 255.
 __device__ __forceinline__ float pow2(int biased) {
     const uint32_t bits = biased == 0 ? 0x00400000u : biased == 255 ? 0x7fffffffu : uint32_t(biased) << 23;

@@ -5,6 +5,7 @@
 
 #include "costa_internal.h"
 #include "mx_device.cuh"
+#include "mx_host.h"
 
 namespace costa {
 namespace mx {
@@ -47,7 +48,7 @@ Groups groups_of(int64_t rows, int64_t gpr) {
     return g;
 }
 
-unsigned blocks_for(const Groups &g) { return static_cast<unsigned>(mx_ceil(g.total, kThreads)); }
+int64_t blocks_for(const Groups &g) { return mx_ceil(g.total, kThreads); }
 
 template <typename T> struct Dense {
     T *p;
@@ -307,8 +308,10 @@ template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) quantize_n_kernel(Dense<const T> X, Codes Q, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
+    let_next_start();
     const bool in = gr.at(cols, row, col);
     Sixteen<T> x;
+    after_previous();
     get(X, row, col, cols, stage, x);
     put16<FMT>(Q, in, row, col, cols, x);
 }
@@ -317,8 +320,10 @@ template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> Y, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
+    let_next_start();
     const bool in = gr.at(cols, row, col);
     Sixteen<T> y;
+    after_previous();
     if constexpr (FMT == COSTA_MX_E2M1) {
         uint2 w{};
         __nv_bfloat162 unit = e2m1_unit(0);
@@ -386,6 +391,8 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, block = warp % 4, left = warp / 4 * 64;
     const int64_t r0 = int64_t(blockIdx.x / col_tiles) * kTile, c0 = int64_t(blockIdx.x % col_tiles) * kTile;
     const int in_rows = static_cast<int>(max(int64_t(0), min(int64_t(32), rows - r0 - 32 * block)));
+    let_next_start();
+    after_previous();
     if (sizeof(T) == 2 && pairs) {
         const int64_t c = c0 + left + 2 * lane;
         const T *p = X.p + (r0 + 32 * block) * X.ld + c;
@@ -533,8 +540,10 @@ __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T>
                                                                Codes QG, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
+    let_next_start();
     const bool in = gr.at(cols, row, col);
     Sixteen<T> x, g, y;
+    after_previous();
     get(X, row, col, cols, stage, x);
     if constexpr (GATED) get(G, row, col, cols, stage, g);
 #pragma unroll
@@ -549,9 +558,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) act_backward
                                                                 Dense<T> dG, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
     int64_t row, col;
+    let_next_start();
     const bool in = gr.at(cols, row, col);
     Sixteen<T> d, dx, dg;
     Coded x{}, g{};
+    after_previous();
     if (in) {
         x.load(QX, row, col);
         if constexpr (GATED) g.load(QG, row, col);
@@ -579,50 +590,22 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) act_backward
     if constexpr (GATED) put(dG, row, col, cols, stage, dg);
 }
 
-cudaError_t launched() {
-    const cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) count_launch();
-    return e;
-}
-
 template <typename T, int ACT>
 cudaError_t forward(const costa_mx_dense &X, const costa_mx_dense *G, const costa_mx_dense &Y, const costa_mx_matrix &QX,
                     const costa_mx_matrix *QG, cudaStream_t s) {
     const Groups gr = groups(QX, false);
-    if (G)
-        act_forward_kernel<T, ACT, true><<<blocks_for(gr), kThreads, 0, s>>>(
-            dense<const T>(X), dense<const T>(*G), dense<T>(Y), codes(QX), codes(*QG), X.cols, gr);
-    else
-        act_forward_kernel<T, ACT, false><<<blocks_for(gr), kThreads, 0, s>>>(dense<const T>(X), {}, dense<T>(Y),
-                                                                              codes(QX), {}, X.cols, gr);
-    return launched();
+    return mx_launch(G ? act_forward_kernel<T, ACT, true> : act_forward_kernel<T, ACT, false>, blocks_for(gr), kThreads, 0,
+                     1, s, dense<const T>(X), G ? dense<const T>(*G) : Dense<const T>{}, dense<T>(Y), codes(QX),
+                     QG ? codes(*QG) : Codes{}, X.cols, gr);
 }
 
 template <typename T, int ACT>
 cudaError_t backward(const costa_mx_matrix &QX, const costa_mx_matrix *QG, const costa_mx_dense &dY,
                      const costa_mx_dense &dX, const costa_mx_dense *dG, cudaStream_t s) {
     const Groups gr = groups(QX, false);
-    if (QG)
-        act_backward_kernel<T, ACT, true><<<blocks_for(gr), kThreads, 0, s>>>(
-            codes(QX), codes(*QG), dense<const T>(dY), dense<T>(dX), dense<T>(*dG), dY.cols, gr);
-    else
-        act_backward_kernel<T, ACT, false><<<blocks_for(gr), kThreads, 0, s>>>(
-            codes(QX), {}, dense<const T>(dY), dense<T>(dX), {}, dY.cols, gr);
-    return launched();
-}
-
-template <typename T, int FMT>
-cudaError_t quantize_t(const costa_mx_dense &X, const costa_mx_matrix *QN, const costa_mx_matrix &QT, cudaStream_t s) {
-    const unsigned col_tiles = static_cast<unsigned>(mx_ceil(X.cols, kTile));
-    const unsigned grid = static_cast<unsigned>(col_tiles * mx_ceil(X.rows, kTile));
-    const bool pairs = reinterpret_cast<uint64_t>(X.ptr) % 4 == 0 && X.ld % 2 == 0;
-    if (QN)
-        quantize_t_kernel<T, FMT, true>
-            <<<grid, kThreads, 0, s>>>(dense<const T>(X), pairs, X.rows, X.cols, codes(*QN), codes(QT), col_tiles);
-    else
-        quantize_t_kernel<T, FMT, false>
-            <<<grid, kThreads, 0, s>>>(dense<const T>(X), pairs, X.rows, X.cols, {}, codes(QT), col_tiles);
-    return launched();
+    return mx_launch(QG ? act_backward_kernel<T, ACT, true> : act_backward_kernel<T, ACT, false>, blocks_for(gr), kThreads,
+                     0, 1, s, codes(QX), QG ? codes(*QG) : Codes{}, dense<const T>(dY), dense<T>(dX),
+                     dG ? dense<T>(*dG) : Dense<T>{}, dY.cols, gr);
 }
 
 template <typename F> cudaError_t by_type(int type, F f) {
@@ -638,13 +621,8 @@ cudaError_t launch_mx_quantize_n(const costa_mx_dense &X, const costa_mx_matrix 
     return by_type(X.type, [&](auto t) {
         using T = decltype(t);
         const Groups gr = groups(Q, true);
-        if (Q.format == COSTA_MX_E2M1)
-            quantize_n_kernel<T, COSTA_MX_E2M1>
-                <<<blocks_for(gr), kThreads, 0, s>>>(dense<const T>(X), codes(Q), X.cols, gr);
-        else
-            quantize_n_kernel<T, COSTA_MX_I8>
-                <<<blocks_for(gr), kThreads, 0, s>>>(dense<const T>(X), codes(Q), X.cols, gr);
-        return launched();
+        return mx_launch(Q.format == COSTA_MX_E2M1 ? quantize_n_kernel<T, COSTA_MX_E2M1> : quantize_n_kernel<T, COSTA_MX_I8>,
+                         blocks_for(gr), kThreads, 0, 1, s, dense<const T>(X), codes(Q), X.cols, gr);
     });
 }
 
@@ -652,8 +630,12 @@ cudaError_t launch_mx_quantize_t(const costa_mx_dense &X, const costa_mx_matrix 
                                  cudaStream_t s) {
     return by_type(X.type, [&](auto t) {
         using T = decltype(t);
-        return QT.format == COSTA_MX_E2M1 ? quantize_t<T, COSTA_MX_E2M1>(X, QN, QT, s)
-                                          : quantize_t<T, COSTA_MX_I8>(X, QN, QT, s);
+        const int64_t col_tiles = mx_ceil(X.cols, kTile);
+        const bool pairs = reinterpret_cast<uint64_t>(X.ptr) % 4 == 0 && X.ld % 2 == 0, e2m1 = QT.format == COSTA_MX_E2M1;
+        return mx_launch(QN ? (e2m1 ? quantize_t_kernel<T, COSTA_MX_E2M1, true> : quantize_t_kernel<T, COSTA_MX_I8, true>)
+                            : (e2m1 ? quantize_t_kernel<T, COSTA_MX_E2M1, false> : quantize_t_kernel<T, COSTA_MX_I8, false>),
+                         col_tiles * mx_ceil(X.rows, kTile), kThreads, 0, 1, s, dense<const T>(X), pairs, X.rows, X.cols,
+                         QN ? codes(*QN) : Codes{}, codes(QT), static_cast<unsigned>(col_tiles));
     });
 }
 
@@ -661,11 +643,8 @@ cudaError_t launch_mx_dequantize(const costa_mx_matrix &Q, const costa_mx_dense 
     return by_type(Y.type, [&](auto t) {
         using T = decltype(t);
         const Groups gr = groups(Q, false);
-        if (Q.format == COSTA_MX_E2M1)
-            dequantize_kernel<T, COSTA_MX_E2M1><<<blocks_for(gr), kThreads, 0, s>>>(codes(Q), dense<T>(Y), Y.cols, gr);
-        else
-            dequantize_kernel<T, COSTA_MX_I8><<<blocks_for(gr), kThreads, 0, s>>>(codes(Q), dense<T>(Y), Y.cols, gr);
-        return launched();
+        return mx_launch(Q.format == COSTA_MX_E2M1 ? dequantize_kernel<T, COSTA_MX_E2M1> : dequantize_kernel<T, COSTA_MX_I8>,
+                         blocks_for(gr), kThreads, 0, 1, s, codes(Q), dense<T>(Y), Y.cols, gr);
     });
 }
 

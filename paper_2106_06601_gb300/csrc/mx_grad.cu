@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::warps * 32, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = static_cast<int>(cluster_rank()), half = rank & 1, lead = rank & ~1, part = rank >> 1;
 
+    let_next_start();
     if (threadIdx.x == 0) {
         failed_word = 0;
         for (int s = 0; s < S::stages; ++s) {
@@ -157,6 +158,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::warps * 32, 1)
     cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
+    after_previous();
 
     const int64_t stages_m = (p.m + kTokens - 1) / kTokens;
     const int64_t s_first = stages_m * part / split, s_last = stages_m * (part + 1) / split;
@@ -400,21 +402,8 @@ cudaError_t launch(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alp
     const int64_t pairs = sms / 2;
     int split = 1;
     while (split < 4 && tiles * split * 2 <= pairs && stages >= 4 * split) split *= 2;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(2 * (split > 1 ? tiles * split : std::min(tiles, pairs))));
-    cfg.blockDim = dim3(S::warps * 32);
-    cfg.dynamicSmemBytes = S::smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {static_cast<unsigned>(2 * split), 1, 1};
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaFuncSetAttribute(grad_kernel<NT, SRC, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
-    if (e != cudaSuccess) return e;
-    e = cudaLaunchKernelEx(&cfg, grad_kernel<NT, SRC, T>, x_map, y_map, p, out, split);
-    if (e == cudaSuccess) count_launch();
-    return e;
+    return mx_launch(grad_kernel<NT, SRC, T>, 2 * (split > 1 ? tiles * split : std::min(tiles, pairs)), S::warps * 32,
+                     S::smem, 2 * split, s, x_map, y_map, p, out, split);
 }
 
 template <typename T>

@@ -38,6 +38,8 @@ cudaError_t tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *b
 }
 
 template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t rows, int64_t cols, float beta) {
+    mx::let_next_start();
+    mx::after_previous();
     for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
         for (int64_t j = threadIdx.x; j < cols; j += blockDim.x) {
             T *at = c + i * ld + j;
@@ -62,14 +64,11 @@ cudaError_t mx_scale_map(CUtensorMap *map, const void *base, uint64_t tiles, uin
 }
 
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(C.rows < 65536 ? C.rows : 65536);
+    const int64_t blocks = C.rows < 65536 ? C.rows : 65536;
     if (C.type == COSTA_MX_F32)
-        scale_kernel<<<grid, 256, 0, s>>>(static_cast<float *>(C.ptr), C.ld, C.rows, C.cols, beta);
-    else
-        scale_kernel<<<grid, 256, 0, s>>>(static_cast<__nv_bfloat16 *>(C.ptr), C.ld, C.rows, C.cols, beta);
-    const cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) count_launch();
-    return e;
+        return mx_launch(scale_kernel<float>, blocks, 256, 0, 1, s, static_cast<float *>(C.ptr), C.ld, C.rows, C.cols, beta);
+    return mx_launch(scale_kernel<__nv_bfloat16>, blocks, 256, 0, 1, s, static_cast<__nv_bfloat16 *>(C.ptr), C.ld, C.rows,
+                     C.cols, beta);
 }
 
 }  // namespace costa

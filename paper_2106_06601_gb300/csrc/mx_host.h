@@ -7,8 +7,42 @@
 #include <cuda_runtime_api.h>
 
 #include "costa_gb300.h"
+#include "costa_internal.h"
 
 namespace costa {
+
+// Launches a kernel of the low-bit operators, in clusters of `cluster` blocks,
+// as a dependent of the kernel before it on the stream: its blocks may start
+// when that one's have all started (or, for a kernel that says nothing, ended),
+// set themselves up, and wait in after_previous() until it is complete and its
+// writes are visible.  Measured on GB300, two launches that follow each other
+// (a token's quantisation and its inverse): 3.9 -> 2.4 us each.
+template <typename... P, typename... A>
+cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, size_t smem, int cluster, cudaStream_t s,
+                      A &&...args) {
+    if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim = {static_cast<unsigned>(cluster), 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cudaError_t e = cudaSuccess;
+    if (smem > 48 * 1024)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    if (e == cudaSuccess)
+        count_launch();
+    else
+        cudaGetLastError();
+    return e;
+}
 
 // 2-D tensor maps, zeros outside, 128-byte swizzle: of bytes, `width` bytes x
 // `rows`, `pitch` bytes from row to row, in boxes of 128 bytes x `box_rows`

@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = static_cast<int>(cluster_rank()), half = kPair ? rank & 1 : 0;
 
+    let_next_start();
     if (threadIdx.x == 0) {
         failed_word = 0;
         for (int s = 0; s < S::stages; ++s) {
@@ -99,6 +100,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if constexpr (kPair) cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
+    after_previous();
 
     // This block's share of k, in stages; and its tiles.  (Pairs do not split k.)
     const int stages_k = (p.steps + 3) / 4;
@@ -299,22 +301,9 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     const int stages_k = (p.steps + 3) / 4;
     int split = 1;
     while (!S::pair && split < 8 && tiles * split * 2 <= 2 * sms && stages_k >= 4 * split) split *= 2;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(
-        S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks))));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = S::smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {static_cast<unsigned>(S::blocks * split), 1, 1};
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaFuncSetAttribute(product_kernel<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
-    if (e != cudaSuccess) return e;
-    e = cudaLaunchKernelEx(&cfg, product_kernel<NT, T>, a_map, b_map, a_scale_map, b_scale_map, p, out, split);
-    if (e == cudaSuccess) count_launch();
-    return e;
+    const int64_t blocks = S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks));
+    return mx_launch(product_kernel<NT, T>, blocks, kThreads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
+                     b_scale_map, p, out, split);
 }
 
 template <typename T>
