@@ -56,12 +56,21 @@ __device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w 
 
 // Added to 1.5 2^23 a number below 2^22 is rounded to an integer, to nearest
 // even, in the low bits; they are clamped in pairs of 16 bits.
+__device__ __forceinline__ uint32_t clamp127(uint32_t pair) {
+    asm("min.s16x2 %0, %0, %1;" : "+r"(pair) : "r"(0x007f007fu));
+    asm("max.s16x2 %0, %0, %1;" : "+r"(pair) : "r"(0xff81ff81u));
+    return pair;
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    asm("max.u16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
 __device__ __forceinline__ uint32_t i8_of4(float a, float b, float c, float d, float f) {
     constexpr float kRound = 12582912.0f;
     uint32_t p = __byte_perm(__float_as_uint(fmaf(a, f, kRound)), __float_as_uint(fmaf(b, f, kRound)), 0x5410);
     uint32_t q = __byte_perm(__float_as_uint(fmaf(c, f, kRound)), __float_as_uint(fmaf(d, f, kRound)), 0x5410);
-    p = __vmaxs2(__vmins2(p, 0x007f007fu), 0xff81ff81u);
-    q = __vmaxs2(__vmins2(q, 0x007f007fu), 0xff81ff81u);
+    p = clamp127(p);
+    q = clamp127(q);
     return __byte_perm(p, q, 0x6420);
 }
 template <typename X> __device__ __forceinline__ uint2 i8_of8(const X &x, int s) {
@@ -118,27 +127,64 @@ template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// Elements col .. col + 7 of a row of `cols`, 0 past its end.  vec: row + col
-// is 16-byte aligned.
-template <typename T>
-__device__ __forceinline__ void load8(const T *row, int64_t col, int64_t cols, bool vec, float (&x)[8]) {
-    if (vec && col + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4 *>(row + col), b = *reinterpret_cast<const float4 *>(row + col + 4);
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4 *>(row + col);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// N elements of T from p, which need not be aligned, as words.  load() brings
+// the whole 16-byte chunks that hold one of the first `count`; place() shifts
+// them into place and clears the elements after those.
+template <typename T, int N> struct Unaligned {
+    static constexpr int kWords = N * sizeof(T) / 4;
+    uint32_t c[kWords + 4];
+    __device__ static uint32_t offset(const T *p) { return static_cast<uint32_t>(reinterpret_cast<uint64_t>(p)) & 15; }
+    __device__ void load(const T *p, uint32_t off, int count) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) - off);
+        const int bytes = count > 0 ? static_cast<int>(off) + count * static_cast<int>(sizeof(T)) : 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int j = 0; j <= kWords / 4; ++j) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (16 * j < bytes) v = from[j];
+            c[4 * j] = v.x;
+            c[4 * j + 1] = v.y;
+            c[4 * j + 2] = v.z;
+            c[4 * j + 3] = v.w;
+        }
+    }
+    __device__ void load_whole(const T *p, uint32_t off) {  // all N exist
+        const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) - off);
+#pragma unroll
+        for (int j = 0; j <= kWords / 4; ++j) {
+            if (j == kWords / 4 && off == 0) break;
+            const uint4 v = from[j];
+            c[4 * j] = v.x;
+            c[4 * j + 1] = v.y;
+            c[4 * j + 2] = v.z;
+            c[4 * j + 3] = v.w;
+        }
+    }
+    __device__ void place(uint32_t off, int count, uint32_t (&w)[kWords]) {
+        if (off != 0) {
+#pragma unroll
+            for (int i = 0; i < kWords + 2; ++i) c[i] = off & 8 ? c[i + 2] : c[i];
+#pragma unroll
+            for (int i = 0; i < kWords + 1; ++i) c[i] = off & 4 ? c[i + 1] : c[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            w[i] = sizeof(T) == 2 && off != 0 ? __funnelshift_r(c[i], c[i + 1], (off & 2) * 8) : c[i];
+        if (count >= N) return;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 2) {
+                if (2 * i >= count) w[i] = 0;
+                if (2 * i + 1 >= count) w[i] &= 0xffffu;
+            } else {
+                if (i >= count) w[i] = 0;
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = col + i < cols ? to_float(row[col + i]) : 0.0f;
     }
+};
+
+// How many of the `n` elements from column `col` a row of `cols` has.
+__device__ __forceinline__ int count_from(int64_t col, int64_t cols, int n) {
+    return static_cast<int>(max(int64_t(0), min(int64_t(n), cols - col)));
 }
 
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {

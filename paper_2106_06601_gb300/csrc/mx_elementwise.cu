@@ -95,7 +95,7 @@ template <> struct Sixteen<__nv_bfloat16> {
     __device__ int exponent() const {
         uint32_t a = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a = __vmaxu2(a, w[i] & 0x7fff7fffu);
+        for (int i = 0; i < 8; ++i) a = max_u16x2(a, w[i] & 0x7fff7fffu);
         return max(a & 0xffffu, a >> 16) >> 7;
     }
     __device__ uint2 e2m1(float f) const {
@@ -124,34 +124,55 @@ __device__ __forceinline__ void store32(void *p, const uint32_t *w) {
                  : "memory");
 }
 
-// The elements of a warp's 32 groups where rows are not aligned or end inside a
-// group: the lanes take a block's 32 elements together, through 2 KB of shared
-// memory of the warp.  Lane 2 i holds block i's place and how many of its
-// elements exist; in most warps all blocks follow each other in a row.
+// This thread's 16 elements, 0 past the row's end.
+template <typename T>
+__device__ __forceinline__ void get(const Dense<const T> &X, int64_t row, int64_t col, int64_t cols, Sixteen<T> &x) {
+    constexpr int kWords = sizeof(x.w) / 4;
+    const T *p = X.p + row * X.ld + col;
+    const int count = count_from(col, cols, 16);
+    if (X.align == 2 && count == 16) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 8) load32(reinterpret_cast<const char *>(p) + 4 * i, x.w + i);
+    } else if (X.align == 1 && count == 16) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4)
+            *reinterpret_cast<uint4 *>(x.w + i) = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
+    } else {
+        Unaligned<T, 16> u;
+        const uint32_t off = u.offset(p);
+        u.load(p, off, count);
+        u.place(off, count, x.w);
+    }
+}
+
+// The elements of a warp's 32 groups on their way to rows that are not aligned
+// or end inside a group: the lanes write a block's 32 elements together, from 2
+// KB of shared memory of the warp.  Lane 2 i holds block i's place and how many
+// of its elements exist; in most warps all blocks follow each other in a row.
 struct Blocks {
     int64_t place, first;
     int count, left;
     bool run;
     __device__ Blocks(int64_t row, int64_t col, int64_t cols, int64_t ld)
-        : place(row * ld + col), count(static_cast<int>(max(int64_t(0), min(int64_t(32), cols - col)))) {
+        : place(row * ld + col), count(count_from(col, cols, 32)) {
         const int lane = threadIdx.x % 32;
         first = __shfl_sync(~0u, place, 0);
         run = __all_sync(~0u, place == first + 16 * lane || count == 0);
         // elements from the first on: whole blocks, then one that may end, then none
         left = __reduce_add_sync(~0u, lane % 2 ? 0 : count);
     }
-    // f(i, place) for this lane's element of blocks from .. from + N - 1, where it exists.
-    template <int N, typename F> __device__ void each(int from, F f) const {
+    // f(i, place) for this lane's element of each block i, where it exists.
+    template <typename F> __device__ void each(F f) const {
         const int lane = threadIdx.x % 32;
         if (run) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (32 * (from + i) + lane < left) f(i, first + lane + 32 * (from + i));
+            for (int i = 0; i < 16; ++i)
+                if (32 * i + lane < left) f(i, first + lane + 32 * i);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int64_t p = __shfl_sync(~0u, place, 2 * (from + i));
-                if (lane < __shfl_sync(~0u, count, 2 * (from + i))) f(i, p + lane);
+            for (int i = 0; i < 16; ++i) {
+                const int64_t p = __shfl_sync(~0u, place, 2 * i);
+                if (lane < __shfl_sync(~0u, count, 2 * i)) f(i, p + lane);
             }
         }
     }
@@ -165,49 +186,7 @@ __device__ __forceinline__ int element_at(int i, int lane) {
     return 32 * i + (lane & 16) + 4 * ((lane >> 2 & 3) ^ (i & 3)) + (lane & 3);
 }
 
-// This thread's 16 elements, 0 past the row's end.  Whole warps call this.
-template <typename T>
-__device__ __forceinline__ void get(const Dense<const T> &X, int64_t row, int64_t col, int64_t cols, float *stage,
-                                    Sixteen<T> &x) {
-    constexpr int kWords = sizeof(x.w) / 4;
-    if (X.align && __all_sync(~0u, col + 16 <= cols || col >= cols)) {
-        if (col >= cols) {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) x.w[i] = 0;
-            return;
-        }
-        const T *p = X.p + row * X.ld + col;
-        if (X.align == 2) {
-#pragma unroll
-            for (int i = 0; i < kWords; i += 8) load32(reinterpret_cast<const char *>(p) + 4 * i, x.w + i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kWords; i += 4)
-                *reinterpret_cast<uint4 *>(x.w + i) = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
-        }
-        return;
-    }
-    const int lane = threadIdx.x % 32;
-    const Blocks b(row, col, cols, X.ld);
-    __syncwarp();
-#pragma unroll
-    for (int h = 0; h < 16; h += 8) {
-        float v[8] = {};
-        b.each<8>(h, [&](int i, int64_t at) { v[i] = to_float(X.p[at]); });
-#pragma unroll
-        for (int i = 0; i < 8; ++i) stage[element_at(h + i, lane)] = v[i];
-    }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(stage + four_at(lane, i / 4));
-        x.set(i, v.x);
-        x.set(i + 1, v.y);
-        x.set(i + 2, v.z);
-        x.set(i + 3, v.w);
-    }
-}
-
+// Writes this thread's 16 elements, those of the row.  Whole warps call this.
 template <typename T>
 __device__ __forceinline__ void put(const Dense<T> &Y, int64_t row, int64_t col, int64_t cols, float *stage,
                                     const Sixteen<T> &x) {
@@ -231,7 +210,7 @@ __device__ __forceinline__ void put(const Dense<T> &Y, int64_t row, int64_t col,
     for (int i = 0; i < 16; i += 4)
         *reinterpret_cast<float4 *>(stage + four_at(lane, i / 4)) = make_float4(x(i), x(i + 1), x(i + 2), x(i + 3));
     __syncwarp();
-    b.each<16>(0, [&](int i, int64_t at) { Y.p[at] = from_float<T>(stage[element_at(i, lane)]); });
+    b.each([&](int i, int64_t at) { Y.p[at] = from_float<T>(stage[element_at(i, lane)]); });
 }
 
 #define COSTA_MX_STAGE                                        \
@@ -306,13 +285,12 @@ Groups groups(const costa_mx_matrix &q, bool tiles) {
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) quantize_n_kernel(Dense<const T> X, Codes Q, int64_t cols, Groups gr) {
-    COSTA_MX_STAGE;
     int64_t row, col;
     let_next_start();
     const bool in = gr.at(cols, row, col);
     Sixteen<T> x;
     after_previous();
-    get(X, row, col, cols, stage, x);
+    get(X, row, col, cols, x);
     put16<FMT>(Q, in, row, col, cols, x);
 }
 
@@ -387,7 +365,6 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
     constexpr int kBlockBytes = FMT == COSTA_MX_E2M1 ? 16 : 32, kPitch = 4 * kBlockBytes + 16;
     __shared__ __align__(16) uint8_t codes[kTile * kPitch];
     __shared__ __align__(16) uint8_t sc[2][kTile][4];
-    COSTA_MX_STAGE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, block = warp % 4, left = warp / 4 * 64;
     const int64_t r0 = int64_t(blockIdx.x / col_tiles) * kTile, c0 = int64_t(blockIdx.x % col_tiles) * kTile;
     const int in_rows = static_cast<int>(max(int64_t(0), min(int64_t(32), rows - r0 - 32 * block)));
@@ -407,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
                 v[i] = *reinterpret_cast<const uint16_t *>(p);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) a = __vmaxu2(a, v[i] & 0x7fff7fffu);
+        for (int i = 0; i < 32; ++i) a = max_u16x2(a, v[i] & 0x7fff7fffu);
         const int sc2[2] = {scale_byte<FMT>((a & 0xffffu) >> 7), scale_byte<FMT>(a >> 23)};
         if constexpr (FMT == COSTA_MX_E2M1) {
             const __nv_bfloat162 f = __floats2bfloat162_rn(e2m1_factor(sc2[0]), e2m1_factor(sc2[1]));
@@ -473,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int64_t row = r0 + 16 * warp + 4 * (i + k) + lane / 8;
-                get(X, min(row, rows - 1), row < rows ? col : cols, cols, stage, y[k]);
+                get(X, min(row, rows - 1), row < rows ? col : cols, cols, y[k]);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -544,8 +521,8 @@ __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T>
     const bool in = gr.at(cols, row, col);
     Sixteen<T> x, g, y;
     after_previous();
-    get(X, row, col, cols, stage, x);
-    if constexpr (GATED) get(G, row, col, cols, stage, g);
+    get(X, row, col, cols, x);
+    if constexpr (GATED) get(G, row, col, cols, g);
 #pragma unroll
     for (int i = 0; i < 16; ++i) y.set(i, GATED ? act<ACT>(x(i)) * g(i) : act<ACT>(x(i)));
     put(Y, row, col, cols, stage, y);
@@ -567,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) act_backward
         x.load(QX, row, col);
         if constexpr (GATED) g.load(QG, row, col);
     }
-    get(dY, row, col, cols, stage, d);
+    get(dY, row, col, cols, d);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float xs[4], gs[4];

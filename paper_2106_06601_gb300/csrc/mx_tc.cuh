@@ -42,12 +42,16 @@ __device__ __forceinline__ void bar_arrive_at(uint32_t bar, uint32_t rank) {
         "r"(rank)
         : "memory");
 }
+// Whether the phase of this parity is complete; the thread may be suspended for
+// some milliseconds until it is (a thread that asks again and again takes issue
+// slots from the others).
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t p;
     asm volatile(
-        "{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        "{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(p)
-        : "r"(bar), "r"(parity)
+        : "r"(bar), "r"(parity), "r"(4000000u)
         : "memory");
     return p != 0;
 }
@@ -62,21 +66,21 @@ constexpr long long kWaitClocks = 8000000000ll;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
     if (bar_try(bar, parity)) return true;
     const long long start = clock64();
-    for (uint32_t i = 1;; ++i) {
-        if (bar_try(bar, parity)) return true;
-        if ((i & 63) == 0 && (*failed || clock64() - start > kWaitClocks)) break;
-    }
-    *failed = 1;
-    return false;
+    while (!bar_try(bar, parity))
+        if (*failed || clock64() - start > kWaitClocks) {
+            *failed = 1;
+            return false;
+        }
+    return true;
 }
 
 // A place in a ring of N stages and the parity of its barriers' current phase.
 template <int N> struct Ring {
     int s = 0;
     uint32_t parity = 0;
-    __device__ void next() {
-        if (++s == N) {
-            s = 0;
+    __device__ void next(int steps = 1) {  // fewer than N
+        if ((s += steps) >= N) {
+            s -= N;
             parity ^= 1;
         }
     }
