@@ -655,7 +655,12 @@ costa_status costa_phase_times(double *ms, int *nphases);
  *    to the output's type.  Repeated calls give the same bits.
  *  - Empty matrices are allowed (rows or columns 0; null pointers then).
  *  - Storage: memory that the current device can address, as for costa_block;
- *    first and last byte of each matrix are checked (COSTA_ERR_LAYOUT). */
+ *    every call checks it, from the first to the last byte of each matrix
+ *    (COSTA_ERR_LAYOUT).  Dense inputs whose rows are not 16-byte aligned may
+ *    be read in whole aligned 16-byte chunks, as costa_block's source runs.
+ *    Outputs are written element by element; nothing outside them is.
+ *  - Kernels start as programmatic dependents of the kernel before them on the
+ *    stream; they read and write nothing until it is complete. */
 
 /* Element types of dense matrices. */
 typedef enum { COSTA_MX_F32 = 0, COSTA_MX_BF16 = 1 } costa_mx_type;

@@ -96,28 +96,34 @@ AttrsFn attrs_fn() {
     return fn;
 }
 
-// Whether the current device can address the bytes [p, p + bytes), which lie in one allocation.
+// Whether the current device can address the bytes [p, p + bytes): in one
+// allocation, or in mappings that follow each other without a gap (as a pool
+// that grows by mapping more memory has).
 costa_status check_bytes(const void *p, int64_t bytes, int dev, const char *name) {
     AttrsFn fn = attrs_fn();
     if (!fn) return bad(COSTA_ERR_CUDA, "no CUDA driver");
-    unsigned int type = 0, managed = 0;
-    int ordinal = -1;
-    CUdeviceptr start = 0, on_device = 0;
-    size_t size = 0;
-    CUpointer_attribute what[6] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE,      CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
-                                   CU_POINTER_ATTRIBUTE_RANGE_START_ADDR, CU_POINTER_ATTRIBUTE_RANGE_SIZE,
-                                   CU_POINTER_ATTRIBUTE_IS_MANAGED,       CU_POINTER_ATTRIBUTE_DEVICE_POINTER};
-    void *out[6] = {&type, &ordinal, &start, &size, &managed, &on_device};
-    const CUdeviceptr a = reinterpret_cast<CUdeviceptr>(p);
-    const CUresult r = fn(6, what, out, a);
-    if (r != CUDA_SUCCESS || type == 0)
-        return bad(COSTA_ERR_LAYOUT, "%s: pageable host memory or an address unknown to CUDA", name);
-    if (type == CU_MEMORYTYPE_DEVICE && !managed && ordinal != dev)
-        return bad(COSTA_ERR_LAYOUT, "%s: memory of device %d, not of the current device %d", name, ordinal, dev);
-    if (type == CU_MEMORYTYPE_HOST && on_device != a)
-        return bad(COSTA_ERR_LAYOUT, "%s: host memory not mapped at the same address on the device", name);
-    if (size > 0 && (a < start || static_cast<uint64_t>(bytes) > start + size - a))
-        return bad(COSTA_ERR_LAYOUT, "%s: %lld bytes from its pointer leave the allocation", name, (long long)bytes);
+    CUdeviceptr a = reinterpret_cast<CUdeviceptr>(p);
+    const CUdeviceptr end = a + static_cast<uint64_t>(bytes);
+    for (int mappings = 0; a < end; ++mappings) {
+        unsigned int type = 0, managed = 0;
+        int ordinal = -1;
+        CUdeviceptr start = 0, on_device = 0;
+        size_t size = 0;
+        CUpointer_attribute what[6] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE,      CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
+                                       CU_POINTER_ATTRIBUTE_RANGE_START_ADDR, CU_POINTER_ATTRIBUTE_RANGE_SIZE,
+                                       CU_POINTER_ATTRIBUTE_IS_MANAGED,       CU_POINTER_ATTRIBUTE_DEVICE_POINTER};
+        void *out[6] = {&type, &ordinal, &start, &size, &managed, &on_device};
+        const bool known = fn(6, what, out, a) == CUDA_SUCCESS && type != 0;
+        if (!known && mappings == 0)
+            return bad(COSTA_ERR_LAYOUT, "%s: pageable host memory or an address unknown to CUDA", name);
+        if (!known || size == 0 || a < start || a >= start + size || mappings > 65536)
+            return bad(COSTA_ERR_LAYOUT, "%s: %lld bytes from its pointer leave the allocation", name, (long long)bytes);
+        if (type == CU_MEMORYTYPE_DEVICE && !managed && ordinal != dev)
+            return bad(COSTA_ERR_LAYOUT, "%s: memory of device %d, not of the current device %d", name, ordinal, dev);
+        if (type == CU_MEMORYTYPE_HOST && on_device != a)
+            return bad(COSTA_ERR_LAYOUT, "%s: host memory not mapped at the same address on the device", name);
+        a = start + size;
+    }
     return COSTA_OK;
 }
 

@@ -30,6 +30,7 @@ namespace {
 constexpr int kCols = 128;     // columns of X in a block's half of a tile
 constexpr int kTokens = 64;    // of a stage
 constexpr int kProducts = 32;  // to a sum in tensor memory
+constexpr int kMaxSplit = 4;
 
 __device__ unsigned g_failed;
 
@@ -209,6 +210,12 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
                 }
             }
         }
+        if (split > 1) {  // one tile to a cluster
+            __syncwarp();
+            cluster_sync();  // (the other warps do so below)
+            join_split<kMaxSplit>(out, ring, half, 2, part, split, threadIdx.x, 256, int64_t(first / p.k_tiles) * NT,
+                                  int64_t(first % p.k_tiles) * (2 * kCols) + half * kCols, NT);
+        }
     } else if (warp < 12) {
         fewer_registers<S::for_copies>();
         if (warp == 8) {  // dY as it is
@@ -377,9 +384,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
     __syncwarp();
 
     if (*failed) let_copies_land();
-    if (split > 1)  // one tile to a cluster
-        join_split(out, ring, half, 2, part, split, int64_t(first / p.k_tiles) * NT,
-                   int64_t(first % p.k_tiles) * (2 * kCols) + half * kCols, NT);
+    if (split > 1 && warp >= 8) cluster_sync();
     fence_before();
     __syncthreads();
     cluster_sync();  // neither block leaves, or frees tensor memory, while the other's products run
@@ -416,7 +421,7 @@ cudaError_t launch(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alp
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     const int64_t pairs = sms / 2;
     int split = 1;
-    while (split < 4 && tiles * split * 2 <= pairs && stages >= 4 * split) split *= 2;
+    while (split < kMaxSplit && tiles * split * 2 <= pairs && stages >= 4 * split) split *= 2;
     return mx_launch(grad_kernel<NT, SRC, T>, 2 * (split > 1 ? tiles * split : std::min(tiles, pairs)),
                      S::groups * 128, S::smem, 2 * split, s, y_map, p, out, split);
 }

@@ -19,6 +19,8 @@ namespace {
 
 constexpr int kThreads = 192;
 constexpr int kRows = 128;  // rows of B in a block's tile
+constexpr int kPrefetch = 4;  // stages of B on their way to the L2 early (0, 4, 8, 16: 1 x 16384 x 4096 10.5, 9.8, 10.1, 10.1 us)
+constexpr int kMaxSplit = 8;
 // A stage holds 256 elements of k: 128 bytes of a row, 2 tiles of scales.
 
 __device__ unsigned g_failed;
@@ -100,7 +102,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     if constexpr (kPair) cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
-    after_previous();
 
     // This block's share of k, in stages; and its tiles.  (Pairs do not split k.)
     const int stages_k = (p.steps + 3) / 4;
@@ -108,6 +109,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int k_first = static_cast<int>(int64_t(stages_k) * part / split);
     const int k_last = static_cast<int>(int64_t(stages_k) * (part + 1) / split);
     const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / per_tile, stride = gridDim.x / per_tile;
+    // Few rows of A: the time is that of reading B, which starts while the kernel before this one ends.
+    if (NT <= 64 && warp == 4 && first < tiles && elect_one())
+        for (int k = k_first; k < min(k_last, k_first + kPrefetch); ++k)
+            tma_prefetch_2d(&b_map, k * 128, first / p.m_tiles * kRows);
+    __syncwarp();
+    after_previous();
 
     if (warp == 4) {
         if (elect_one()) {
@@ -253,8 +260,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
 
     if (*failed) let_copies_land();
-    if (split > 1)  // one tile to a cluster
-        join_split(out, ring, 0, 1, part, split, int64_t(first % p.m_tiles) * NT, int64_t(first / p.m_tiles) * kRows, NT);
+    if (split > 1) {  // one tile to a cluster
+        cluster_sync();
+        join_split<kMaxSplit>(out, ring, 0, 1, part, split, threadIdx.x, kThreads, int64_t(first % p.m_tiles) * NT,
+                              int64_t(first / p.m_tiles) * kRows, NT);
+        cluster_sync();
+    }
     fence_before();
     __syncthreads();
     if constexpr (kPair) cluster_sync();  // neither block leaves while the other's products run
@@ -300,7 +311,8 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     const int stages_k = (p.steps + 3) / 4;
     int split = 1;
-    while (!S::pair && split < 8 && tiles * split * 2 <= 2 * sms && stages_k >= 4 * split) split *= 2;
+    const int resident = NT <= 64 ? 2 : 1;  // blocks of an SM, by their shared memory
+    while (!S::pair && split < kMaxSplit && tiles * split * 2 <= resident * sms && stages_k >= 4 * split) split *= 2;
     const int64_t blocks = S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks));
     return mx_launch(product_kernel<NT, T>, blocks, kThreads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
                      b_scale_map, p, out, split);
@@ -312,8 +324,12 @@ cudaError_t by_rows(const costa_mx_matrix &A, const costa_mx_matrix &B, float al
     if (C.rows <= 16) return launch<16, T>(A, B, alpha, beta, C, sms, s);
     if (C.rows <= 32) return launch<32, T>(A, B, alpha, beta, C, sms, s);
     if (C.rows <= 64) return launch<64, T>(A, B, alpha, beta, C, sms, s);
-    if (C.rows <= 128 || mx_ceil(C.rows, 256) * mx_ceil(C.cols, 256) < sms / 2)
-        return launch<128, T>(A, B, alpha, beta, C, sms, s);
+    // A round of tiles of 256 x 256 on all pairs takes 1.26 times as long as one of 128 x 128 on all SMs (1100 x 4096 x
+    // 4096, two rounds of either: 20.7 and 17.5 us with the quantisation; 768 rows, one round and two: 13.7, 16.5;
+    // 512 rows, one of either: 12.9, 10.9; 2048 rows, two and four: 23.1, 29.3).
+    const int64_t small = mx_ceil(mx_ceil(C.rows, 128) * mx_ceil(C.cols, 128), sms),
+                  large = mx_ceil(mx_ceil(C.rows, 256) * mx_ceil(C.cols, 256), sms / 2);
+    if (C.rows <= 128 || 4 * small <= 5 * large) return launch<128, T>(A, B, alpha, beta, C, sms, s);
     return launch<256, T>(A, B, alpha, beta, C, sms, s);
 }
 

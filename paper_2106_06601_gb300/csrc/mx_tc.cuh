@@ -100,6 +100,10 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// The same box only as far as the L2: no data reach the block, so this may run before after_previous().
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap *map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 // The same, counted at the barrier of block `rank` (of this pair of blocks).
 __device__ __forceinline__ void tma_load_2d_at(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar,
                                                uint32_t rank) {
@@ -241,11 +245,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ float4 cluster_load(uint32_t addr, uint32_t rank) {
     uint32_t a;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
     return v;
 }
 
@@ -281,21 +285,44 @@ template <typename T> struct Output {
     }
 };
 
-// Joins the partial sums of `split` blocks of a cluster (at shared address
-// `part` of the blocks first, first + step, ...), in that order; each of them,
-// the index-th, writes a share.  All threads of the cluster call this.
-template <typename T>
+// Joins the partial sums of `split` <= MAX blocks of a cluster (at shared
+// address `part` of the blocks first, first + step, ...), in that order; each of
+// them, the index-th, writes a share with `threads` threads, of which this is
+// the tid-th.  A cluster_sync() comes before this, and one after it before any
+// block leaves.
+template <int MAX, typename T>
 __device__ __forceinline__ void join_split(const Output<T> &out, uint32_t part, int first, int step, int index, int split,
-                                           int64_t row0, int64_t col0, int tile_rows) {
-    __syncwarp();
-    cluster_sync();
-    const int total = static_cast<int>(min(int64_t(tile_rows), out.rows - row0)) * 128;
-    for (int e = index * blockDim.x + threadIdx.x; e < total; e += split * blockDim.x) {
-        float v = 0.0f;
-        for (int r = 0; r < split; ++r) v += cluster_load(part + 4 * e, first + r * step);
-        if (col0 + e % 128 < out.cols) out.put(row0 + e / 128, col0 + e % 128, v);
+                                           int tid, int threads, int64_t row0, int64_t col0, int tile_rows) {
+    // Four neighbouring columns at a time, and two such groups of all blocks on their way together: another block's
+    // shared memory is some 700 cycles away.
+    const int groups = static_cast<int>(min(int64_t(tile_rows), out.rows - row0)) * 32, stride = split * threads;
+    for (int g = index * threads + tid; g < groups; g += 2 * stride) {
+        float4 v[2][MAX];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < MAX; ++r)
+                if (r < split && g + h * stride < groups) v[h][r] = cluster_load(part + 16 * (g + h * stride), first + r * step);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = g + h * stride;
+            if (at >= groups) break;
+            float4 sum = v[h][0];
+#pragma unroll
+            for (int r = 1; r < MAX; ++r)
+                if (r < split) {
+                    sum.x += v[h][r].x;
+                    sum.y += v[h][r].y;
+                    sum.z += v[h][r].z;
+                    sum.w += v[h][r].w;
+                }
+            const int64_t row = row0 + at / 32, col = col0 + at % 32 * 4;
+            const float each[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < out.cols) out.put(row, col + i, each[i]);
+        }
     }
-    cluster_sync();  // no block leaves while others read its sums
 }
 
 }  // namespace mx

@@ -154,7 +154,8 @@ def test_quantize_special_values(fmt, dtype):
 
 PRODUCTS = [(1, 1, 1), (1, 128, 32), (1, 300, 64), (2, 7, 33), (3, 130, 96), (8, 64, 128), (13, 501, 2200), (17, 129, 160),
             (64, 64, 64), (127, 255, 257), (128, 128, 1024), (129, 257, 4096), (200, 1000, 777), (300, 520, 8200),
-            (1000, 33, 513), (5, 4096, 31), (16, 256, 16384), (513, 7000, 160), (700, 13000, 1100)]
+            (1000, 33, 513), (5, 4096, 31), (16, 256, 16384), (513, 7000, 160), (700, 13000, 1100),
+            (750, 4090, 96), (260, 2048, 4100), (90, 16000, 700)]
 
 
 @pytest.mark.parametrize("m, n, k", PRODUCTS)
