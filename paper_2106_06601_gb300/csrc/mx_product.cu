@@ -3,9 +3,10 @@
 //
 // One thread block takes a tile of 128 rows of B (the lanes of tensor memory)
 // and NT rows of A (its columns), so that a warp's lanes hold neighbouring
-// elements of a row of C and few rows of A need few columns.  Warp 4 brings
-// operands and scales into a ring of stages of 256 columns of k, one thread of
-// warp 5 issues the products, warps 0 to 3 write the tile out.  Tiles of 256
+// elements of a row of C and few rows of A need few columns.  The first four or
+// eight warps write the tile out, one or two to a quarter of the lanes; the next
+// brings operands and scales into a ring of stages of 256 columns of k, and one
+// thread of the last issues the products.  Tiles of 256
 // rows of A are taken by pairs of blocks, with 256 rows of B: each block then
 // brings half of A's rows, a third less for the L2 cache to deliver.
 #include <algorithm>
@@ -17,7 +18,6 @@ namespace costa {
 namespace mx {
 namespace {
 
-constexpr int kThreads = 192;
 constexpr int kRows = 128;  // rows of B in a block's tile
 constexpr int kPrefetch = 4;  // stages of B on their way to the L2 early (0, 4, 8, 16: 1 x 16384 x 4096 10.5, 9.8, 10.1, 10.1 us)
 constexpr int kMaxSplit = 8;
@@ -48,6 +48,9 @@ template <int NT> struct Shape {
     static constexpr int used = scales + 2 * scale_cols;
     static constexpr int cols = used <= 64 ? 64 : used <= 128 ? 128 : used <= 256 ? 256 : 512;
     static constexpr int a_rows = NT / blocks;  // in a block
+    // Warps that write a tile out.  Eight would leave registers for one block of an SM, where small tiles have two
+    // (1 x 16384 x 4096 9.7, 14.9 us; 1023 x 4096 x 4096 15.2, 14.2).
+    static constexpr int writers = NT >= 128 ? 8 : 4, threads = (writers + 2) * 32;
     static constexpr int b_bytes = kRows * 128, a_bytes = a_rows * 128, sf_bytes = 1024 * (1 + bands);
     static constexpr int stage = (b_bytes + a_bytes + sf_bytes + 1023) / 1024 * 1024;
     static constexpr int stages = NT == 256 ? 6 : NT == 128 ? 5 : 4;
@@ -56,7 +59,7 @@ template <int NT> struct Shape {
 };
 
 template <int NT, typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<NT>::threads, 1)
     product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                    const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap b_scale_map,
                    const Params p, const Output<T> out, const int split) {
@@ -87,11 +90,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(sum_full(i), 1);
-            bar_init(sum_empty(i), 4 * S::blocks);
+            bar_init(sum_empty(i), S::writers * S::blocks);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 5) {
+    if (warp == S::writers + 1) {
         if constexpr (kPair)
             tmem_alloc_pair(&tmem_slot, S::cols);
         else
@@ -110,13 +113,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int k_last = static_cast<int>(int64_t(stages_k) * (part + 1) / split);
     const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / per_tile, stride = gridDim.x / per_tile;
     // Few rows of A: the time is that of reading B, which starts while the kernel before this one ends.
-    if (NT <= 64 && warp == 4 && first < tiles && elect_one())
+    if (NT <= 64 && warp == S::writers && first < tiles && elect_one())
         for (int k = k_first; k < min(k_last, k_first + kPrefetch); ++k)
             tma_prefetch_2d(&b_map, k * 128, first / p.m_tiles * kRows);
     __syncwarp();
     after_previous();
 
-    if (warp == 4) {
+    if (warp == S::writers) {
         if (elect_one()) {
             Ring<S::stages> at;
             for (int t = first; t < tiles && !*failed; t += stride) {
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
-    } else if (warp == 5) {
+    } else if (warp == S::writers + 1) {
         if (half == 0 && elect_one()) {
             auto commit = [&](uint32_t bar) {
                 if constexpr (kPair)
@@ -201,19 +204,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             fence_after();
             const int nt = t / p.m_tiles, mt = t % p.m_tiles;
             const uint32_t d = tmem + (done & 1 ? S::second : 0);
-            constexpr int kChunks = NT / 16;
-            // the shared columns first: chunks 13 .. 15 of the first sum, 0 .. 2 of the second
-            const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0;
-            const uint32_t lanes = d + (uint32_t(warp * 32) << 16);
+            // Chunks of 16 columns, the warps of a quarter in turn; the shared columns first: chunks 13 .. 15 of the first
+            // sum, 0 .. 2 of the second.
+            constexpr int kChunks = NT / 16, kStep = S::writers / 4;
+            const int shift = kLag == 1 && !(done & 1) ? kChunks - 3 : 0, pick = warp / 4, quarter = warp % 4 * 32;
+            const uint32_t lanes = d + (uint32_t(quarter) << 16);
             const int64_t row0 = int64_t(mt) * NT;
-            const int64_t col = int64_t(nt) * S::rows + half * kRows + warp * 32 + lane;
+            const int64_t col = int64_t(nt) * S::rows + half * kRows + quarter + lane;
             auto load = [&](int j, uint32_t(&r)[16]) { tmem_ld16(lanes + (j + shift) % kChunks * 16, r); };
             auto write = [&](int j, const uint32_t(&r)[16]) {
                 const int ch = (j + shift) % kChunks;
                 if (split > 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        part_sums[(ch * 16 + i) * kRows + warp * 32 + lane] = __uint_as_float(r[i]);
+                    for (int i = 0; i < 16; ++i) part_sums[(ch * 16 + i) * kRows + quarter + lane] = __uint_as_float(r[i]);
                 } else {
                     out.put16(row0 + ch * 16, col, [&](int i) { return __uint_as_float(r[i]); });
                 }
@@ -228,33 +231,32 @@ __global__ void __launch_bounds__(kThreads, 1)
                         bar_arrive(sum_empty(done & 1));
                 }
             };
-            constexpr int kFirst = kLag == 1 ? 3 : 0;  // the shared columns, all read before any is written
+            static_assert(kLag != 1 || 2 * kStep >= 3, "the shared columns are among the first two of each warp");
+            constexpr int kFirst = kLag == 1 ? 2 : 0;  // of a warp, among them the shared columns: read before any is written
             if constexpr (kFirst > 0) {
-                uint32_t r[kFirst][16];
-#pragma unroll
-                for (int j = 0; j < kFirst; ++j) load(j, r[j]);
-#pragma unroll
-                for (int j = 0; j < kFirst; ++j) tmem_wait_ld(r[j]);
+                uint32_t r[2][16];
+                load(pick, r[0]);
+                load(pick + kStep, r[1]);
+                tmem_wait_ld(r[0]);
+                tmem_wait_ld(r[1]);
                 drained();
-#pragma unroll
-                for (int j = 0; j < kFirst; ++j) write(j, r[j]);
+                write(pick, r[0]);
+                write(pick + kStep, r[1]);
             }
             // a chunk is loaded while the one before it is written
             uint32_t r[2][16];
-            load(kFirst, r[0]);
+            load(pick + kStep * kFirst, r[0]);
 #pragma unroll 1
-            for (int j = kFirst; j < kChunks; j += 2) {
+            for (int j = pick + kStep * kFirst; j < kChunks; j += 2 * kStep) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if (j + h >= kChunks) break;
+                    if (j + kStep * h >= kChunks) break;
                     tmem_wait_ld(r[h]);
-                    if (j + h + 1 < kChunks)
-                        load(j + h + 1, r[1 - h]);
-                    else if (kFirst == 0)
-                        drained();
-                    write(j + h, r[h]);
+                    if (j + kStep * (h + 1) < kChunks) load(j + kStep * (h + 1), r[1 - h]);
+                    write(j + kStep * h, r[h]);
                 }
             }
+            if constexpr (kFirst == 0) drained();
         }
     }
     __syncwarp();
@@ -262,14 +264,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (*failed) let_copies_land();
     if (split > 1) {  // one tile to a cluster
         cluster_sync();
-        join_split<kMaxSplit>(out, ring, 0, 1, part, split, threadIdx.x, kThreads, int64_t(first % p.m_tiles) * NT,
+        join_split<kMaxSplit>(out, ring, 0, 1, part, split, threadIdx.x, S::threads, int64_t(first % p.m_tiles) * NT,
                               int64_t(first / p.m_tiles) * kRows, NT);
         cluster_sync();
     }
     fence_before();
     __syncthreads();
     if constexpr (kPair) cluster_sync();  // neither block leaves while the other's products run
-    if (warp == 5) {
+    if (warp == S::writers + 1) {
         fence_after();
         if constexpr (kPair)
             tmem_free_pair(tmem, S::cols);
@@ -314,7 +316,7 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     const int resident = NT <= 64 ? 2 : 1;  // blocks of an SM, by their shared memory
     while (!S::pair && split < kMaxSplit && tiles * split * 2 <= resident * sms && stages_k >= 4 * split) split *= 2;
     const int64_t blocks = S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks));
-    return mx_launch(product_kernel<NT, T>, blocks, kThreads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
+    return mx_launch(product_kernel<NT, T>, blocks, S::threads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
                      b_scale_map, p, out, split);
 }
 
