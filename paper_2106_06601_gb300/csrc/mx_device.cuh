@@ -29,7 +29,16 @@ template <int FMT> __device__ __forceinline__ int scale_byte(int e) {
     return FMT == COSTA_MX_E2M1 ? max(e - 2, 0) : e;
 }
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The larger magnitude (of each half), NaN if there is one: as floating
+// comparisons, which take half the cycles of integer ones and no masking.
+__device__ __forceinline__ float larger(float a, float x) {
+    asm("{\n\t.reg .f32 t;\n\tabs.f32 t, %1;\n\tmax.NaN.f32 %0, %0, t;\n\t}" : "+f"(a) : "f"(x));
+    return a;
+}
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t x) {
+    asm("{\n\t.reg .b32 t;\n\tabs.bf16x2 t, %1;\n\tmax.NaN.bf16x2 %0, %0, t;\n\t}" : "+r"(a) : "r"(x));
+    return a;
+}
 
 // E2M1 codes of 8 numbers x(0) .. x(7), the first in the low bits; the
 // conversion rounds to nearest even and saturates at 6.
@@ -60,10 +69,6 @@ __device__ __forceinline__ uint32_t clamp127(uint32_t pair) {
     asm("min.s16x2 %0, %0, %1;" : "+r"(pair) : "r"(0x007f007fu));
     asm("max.s16x2 %0, %0, %1;" : "+r"(pair) : "r"(0xff81ff81u));
     return pair;
-}
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
-    asm("max.u16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
-    return a;
 }
 __device__ __forceinline__ uint32_t i8_of4(float a, float b, float c, float d, float f) {
     constexpr float kRound = 12582912.0f;

@@ -68,10 +68,10 @@ template <> struct Sixteen<float> {
     __device__ float operator()(int i) const { return __uint_as_float(w[i]); }
     __device__ void set(int i, float x) { w[i] = __float_as_uint(x); }
     __device__ int exponent() const {  // biased, of the largest magnitude
-        uint32_t a = 0;
+        float a = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) a = max(a, w[i] & 0x7fffffffu);
-        return a >> 23;
+        for (int i = 0; i < 16; ++i) a = larger(a, (*this)(i));
+        return __float_as_uint(a) >> 23;
     }
     __device__ uint2 e2m1(float f) const {
         return make_uint2(e2m1_of8([&](int i) { return (*this)(i) * f; }), e2m1_of8([&](int i) { return (*this)(i + 8) * f; }));
@@ -95,7 +95,7 @@ template <> struct Sixteen<__nv_bfloat16> {
     __device__ int exponent() const {
         uint32_t a = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a = max_u16x2(a, w[i] & 0x7fff7fffu);
+        for (int i = 0; i < 8; ++i) a = larger2(a, w[i]);
         return max(a & 0xffffu, a >> 16) >> 7;
     }
     __device__ uint2 e2m1(float f) const {
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
                 v[i] = *reinterpret_cast<const uint16_t *>(p);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) a = max_u16x2(a, v[i] & 0x7fff7fffu);
+        for (int i = 0; i < 32; ++i) a = larger2(a, v[i]);
         const int sc2[2] = {scale_byte<FMT>((a & 0xffffu) >> 7), scale_byte<FMT>(a >> 23)};
         if constexpr (FMT == COSTA_MX_E2M1) {
             const __nv_bfloat162 f = __floats2bfloat162_rn(e2m1_factor(sc2[0]), e2m1_factor(sc2[1]));
@@ -405,12 +405,12 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
             const T *p = X.p + (r0 + 32 * block) * X.ld + c0 + col;
             const int in = c0 + col < cols ? in_rows : 0;
             float x[32];
-            uint32_t a = 0;
+            float a = 0.0f;
 #pragma unroll
             for (int i = 0; i < 32; ++i, p += X.ld) x[i] = i < in ? to_float(*p) : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) a = max(a, magnitude(x[i]));
-            const int s = scale_byte<FMT>(a >> 23);
+            for (int i = 0; i < 32; ++i) a = larger(a, x[i]);
+            const int s = scale_byte<FMT>(__float_as_uint(a) >> 23);
             sc[0][col][block] = static_cast<uint8_t>(s);
             const float f = FMT == COSTA_MX_E2M1 ? e2m1_factor(s) : 1.0f;
             block_codes<FMT>(codes + col * kPitch + block * kBlockBytes, s,
