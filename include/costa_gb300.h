@@ -654,7 +654,7 @@ costa_status costa_phase_times(double *ms, int *nphases);
  *  - Rounding: sums and activations are evaluated in 32 bits and rounded once
  *    to the output's type.  Repeated calls give the same bits.
  *  - Empty matrices are allowed (rows or columns 0; null pointers then).
- *  - Storage: memory that the current device can address, as for costa_block;
+ *  - Storage: memory of the current device (not host or managed memory);
  *    every call checks it, from the first to the last byte of each matrix
  *    (COSTA_ERR_LAYOUT).  Dense inputs whose rows are not 16-byte aligned may
  *    be read in whole aligned 16-byte chunks, as costa_block's source runs.

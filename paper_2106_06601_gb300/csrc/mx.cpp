@@ -96,9 +96,10 @@ AttrsFn attrs_fn() {
     return fn;
 }
 
-// Whether the current device can address the bytes [p, p + bytes): in one
+// Whether the bytes [p, p + bytes) are memory of the current device: in one
 // allocation, or in mappings that follow each other without a gap (as a pool
-// that grows by mapping more memory has).
+// that grows by mapping more memory has).  Host and managed memory is refused:
+// the products' bulk copies take device memory.
 costa_status check_bytes(const void *p, int64_t bytes, int dev, const char *name) {
     AttrsFn fn = attrs_fn();
     if (!fn) return bad(COSTA_ERR_CUDA, "no CUDA driver");
@@ -107,21 +108,20 @@ costa_status check_bytes(const void *p, int64_t bytes, int dev, const char *name
     for (int mappings = 0; a < end; ++mappings) {
         unsigned int type = 0, managed = 0;
         int ordinal = -1;
-        CUdeviceptr start = 0, on_device = 0;
+        CUdeviceptr start = 0;
         size_t size = 0;
-        CUpointer_attribute what[6] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE,      CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
+        CUpointer_attribute what[5] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE, CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
                                        CU_POINTER_ATTRIBUTE_RANGE_START_ADDR, CU_POINTER_ATTRIBUTE_RANGE_SIZE,
-                                       CU_POINTER_ATTRIBUTE_IS_MANAGED,       CU_POINTER_ATTRIBUTE_DEVICE_POINTER};
-        void *out[6] = {&type, &ordinal, &start, &size, &managed, &on_device};
-        const bool known = fn(6, what, out, a) == CUDA_SUCCESS && type != 0;
-        if (!known && mappings == 0)
-            return bad(COSTA_ERR_LAYOUT, "%s: pageable host memory or an address unknown to CUDA", name);
-        if (!known || size == 0 || a < start || a >= start + size || mappings > 65536)
+                                       CU_POINTER_ATTRIBUTE_IS_MANAGED};
+        void *out[5] = {&type, &ordinal, &start, &size, &managed};
+        const bool known = fn(5, what, out, a) == CUDA_SUCCESS && type != 0;
+        if (mappings == 0 && (!known || type != CU_MEMORYTYPE_DEVICE || managed))
+            return bad(COSTA_ERR_LAYOUT, "%s: not device memory", name);
+        if (!known || type != CU_MEMORYTYPE_DEVICE || managed || size == 0 || a < start || a >= start + size ||
+            mappings > 65536)
             return bad(COSTA_ERR_LAYOUT, "%s: %lld bytes from its pointer leave the allocation", name, (long long)bytes);
-        if (type == CU_MEMORYTYPE_DEVICE && !managed && ordinal != dev)
+        if (ordinal != dev)
             return bad(COSTA_ERR_LAYOUT, "%s: memory of device %d, not of the current device %d", name, ordinal, dev);
-        if (type == CU_MEMORYTYPE_HOST && on_device != a)
-            return bad(COSTA_ERR_LAYOUT, "%s: host memory not mapped at the same address on the device", name);
         a = start + size;
     }
     return COSTA_OK;

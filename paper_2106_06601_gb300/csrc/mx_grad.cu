@@ -395,9 +395,35 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
     if (threadIdx.x == 0 && *failed) atomicAdd(&g_failed, 1u);
 }
 
+// How a call is laid out: columns of dY in a tile, and the parts of its tokens.
+struct Layout {
+    int nt, split;
+    double ns;
+};
+
+// The shortest by what was measured: a stage of a pair takes 375 ns with 128
+// columns of dY and 450 with 256, joining the parts some 3 and 6 us, and tiles
+// beyond what the device runs at a time take another round.  (GPU us with the
+// quantisation, 128 and 256 columns: 4096 x 2048 x 2048 55, 36; 4096 x 1024 x
+// 4096 60, 41; 512 x 4096 x 4096 32, 26; 4096 x 1024 x 1024 in two parts 21,
+// in four 32; 4096 x 512 x 512 in four 14, 17.)
+Layout choose(int64_t n, int64_t k, int64_t m, bool wide) {
+    Layout best{128, 1, -1.0};
+    for (int nt = 128; nt <= (wide ? 256 : 128); nt *= 2)
+        for (int split = 1; split <= kMaxSplit; split *= 2) {
+            const int64_t stages = mx_ceil(m, kTokens), tiles = mx_ceil(n, nt) * mx_ceil(k, 2 * kCols);
+            if (split > 1 && stages < 2 * split) break;
+            const double rounds = static_cast<double>(mx_ceil(tiles, mx_clusters(2 * split, 1)));
+            // whole rounds where parts are joined; else pairs go on to the next tile
+            const double ns = rounds * (mx_ceil(stages, split) * (nt == 128 ? 375.0 : 450.0) + (split > 1 ? nt * 24.0 : 0.0));
+            if (best.ns < 0 || ns < best.ns) best = {nt, split, ns};
+        }
+    return best;
+}
+
 template <int NT, int SRC, typename T>
 cudaError_t launch(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alpha, float beta, const costa_mx_dense &dW,
-                   int sms, cudaStream_t s) {
+                   int split, cudaStream_t s) {
     using S = Shape<NT, SRC>;
     CUtensorMap y_map{};
     if (SRC == kDirect) {
@@ -417,23 +443,22 @@ cudaError_t launch(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alp
     p.n_tiles = static_cast<int>(mx_ceil(dY.cols, NT));
     p.k_tiles = static_cast<int>(mx_ceil(Q.cols, 2 * kCols));
     const Output<T> out{static_cast<T *>(dW.ptr), dW.ld, dW.rows, dW.cols, alpha, beta};
-    const int64_t tiles = int64_t(p.n_tiles) * p.k_tiles, stages = mx_ceil(p.m, kTokens);
-    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-    const int64_t pairs = sms / 2;
-    int split = 1;
-    while (split < kMaxSplit && tiles * split * 2 <= pairs && stages >= 4 * split) split *= 2;
-    return mx_launch(grad_kernel<NT, SRC, T>, 2 * (split > 1 ? tiles * split : std::min(tiles, pairs)),
-                     S::groups * 128, S::smem, 2 * split, s, y_map, p, out, split);
+    const int64_t tiles = int64_t(p.n_tiles) * p.k_tiles;
+    if (tiles > INT32_MAX / 16) return cudaErrorInvalidValue;
+    const int64_t pairs = split > 1 ? tiles * split : std::min<int64_t>(tiles, mx_clusters(2, 1));
+    return mx_launch(grad_kernel<NT, SRC, T>, 2 * pairs, S::groups * 128, S::smem, 2 * split, s, y_map, p, out, split);
 }
 
 template <typename T>
 cudaError_t by_source(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alpha, float beta,
-                      const costa_mx_dense &dW, int sms, cudaStream_t s) {
-    if (dY.type == COSTA_MX_F32) return launch<128, kF32, T>(dY, Q, alpha, beta, dW, sms, s);
-    if (reinterpret_cast<uint64_t>(dY.ptr) % 16 || dY.ld % 8) return launch<128, kBf16, T>(dY, Q, alpha, beta, dW, sms, s);
-    if (mx_ceil(dY.cols, 256) * mx_ceil(Q.cols, 2 * kCols) < sms / 2)
-        return launch<128, kDirect, T>(dY, Q, alpha, beta, dW, sms, s);
-    return launch<256, kDirect, T>(dY, Q, alpha, beta, dW, sms, s);
+                      const costa_mx_dense &dW, cudaStream_t s) {
+    const bool f32 = dY.type == COSTA_MX_F32;
+    const bool direct = !f32 && reinterpret_cast<uint64_t>(dY.ptr) % 16 == 0 && dY.ld % 8 == 0;
+    const Layout l = choose(dY.cols, Q.cols, dY.rows, direct);
+    if (f32) return launch<128, kF32, T>(dY, Q, alpha, beta, dW, l.split, s);
+    if (!direct) return launch<128, kBf16, T>(dY, Q, alpha, beta, dW, l.split, s);
+    if (l.nt == 128) return launch<128, kDirect, T>(dY, Q, alpha, beta, dW, l.split, s);
+    return launch<256, kDirect, T>(dY, Q, alpha, beta, dW, l.split, s);
 }
 
 }  // namespace
@@ -442,12 +467,8 @@ cudaError_t by_source(const costa_mx_dense &dY, const costa_mx_matrix &Q, float 
 cudaError_t launch_mx_weight_grad(const costa_mx_dense &dY, const costa_mx_matrix &Q, float alpha, float beta,
                                   const costa_mx_dense &dW, cudaStream_t s) {
     if (dY.rows == 0) return launch_mx_scale(beta, dW, s);
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
-    return dW.type == COSTA_MX_F32 ? mx::by_source<float>(dY, Q, alpha, beta, dW, sms, s)
-                                   : mx::by_source<__nv_bfloat16>(dY, Q, alpha, beta, dW, sms, s);
+    return dW.type == COSTA_MX_F32 ? mx::by_source<float>(dY, Q, alpha, beta, dW, s)
+                                   : mx::by_source<__nv_bfloat16>(dY, Q, alpha, beta, dW, s);
 }
 
 cudaError_t mx_grad_failures(unsigned *count) {

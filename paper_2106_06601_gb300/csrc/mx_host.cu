@@ -1,4 +1,6 @@
 // Host helpers of the low-bit products, and C = beta C.
+#include <atomic>
+
 #include "costa_internal.h"
 #include "mx_device.cuh"
 #include "mx_host.h"
@@ -37,6 +39,9 @@ cudaError_t tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *b
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// Stands for a kernel with as much shared memory in questions about clusters; never launched.
+__global__ void no_kernel() {}
+
 template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t rows, int64_t cols, float beta) {
     mx::let_next_start();
     mx::after_previous();
@@ -61,6 +66,34 @@ cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint6
 
 cudaError_t mx_scale_map(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_tiles) {
     return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, base, 128, tiles, 512, 128, box_tiles, false);
+}
+
+int mx_clusters(int size, int blocks_per_sm) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices][2][4];  // a property of the device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    const int which = size >= 8 ? 3 : size >= 4 ? 2 : size >= 2 ? 1 : 0, two = blocks_per_sm > 1;
+    if (dev < kDevices)
+        if (const int n = known[dev][two][which].load(std::memory_order_relaxed)) return n;
+    const int smem = (two ? 104 : 160) * 1024;
+    int n = 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(size));
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {static_cast<unsigned>(size), 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(no_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, no_kernel, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 1;
+    }
+    if (dev < kDevices) known[dev][two][which].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s) {

@@ -53,6 +53,10 @@ cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint6
                         uint32_t box_rows);
 // Of tiles of scales (512 bytes), in boxes of `box_tiles`, not swizzled.
 cudaError_t mx_scale_map(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_tiles);
+// How many clusters of `size` blocks (1, 2, 4 or 8) the current device runs at a
+// time, with one block to an SM or two: fewer than its SMs would hold, as a
+// cluster stays within one group of SMs (152 SMs: 76 of 2, 36 of 4, 15 of 8).
+int mx_clusters(int size, int blocks_per_sm);
 // C = beta C (0 without reading C for beta == 0): products over nothing.
 cudaError_t launch_mx_scale(float beta, const costa_mx_dense &C, cudaStream_t s);
 // Waits that gave up, on the current device since the library was loaded.

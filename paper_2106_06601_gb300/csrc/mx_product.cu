@@ -312,9 +312,10 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     const int64_t tiles = int64_t(p.n_tiles) * p.m_tiles;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     const int stages_k = (p.steps + 3) / 4;
+    // As many parts of k as run at a time, of two stages at least.
     int split = 1;
-    const int resident = NT <= 64 ? 2 : 1;  // blocks of an SM, by their shared memory
-    while (!S::pair && split < kMaxSplit && tiles * split * 2 <= resident * sms && stages_k >= 4 * split) split *= 2;
+    while (!S::pair && split < kMaxSplit && tiles <= mx_clusters(2 * split, NT <= 64 ? 2 : 1) && stages_k >= 4 * split)
+        split *= 2;
     const int64_t blocks = S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks));
     return mx_launch(product_kernel<NT, T>, blocks, S::threads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
                      b_scale_map, p, out, split);

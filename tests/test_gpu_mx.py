@@ -436,7 +436,9 @@ def test_storage_refusals():
     q = Codes("e2m1", 64, 64)
     n = costa.costa_kernel_launch_count()
     at = -(-host.ctypes.data // 16) * 16
+    pinned = torch.zeros(4096, dtype=torch.uint8).pin_memory()
     for bad in (costa.costa_mx_dense("f32", 4, 64, at, 64),
+                costa.costa_mx_dense("f32", 4, 64, pinned.data_ptr(), 64),
                 costa.costa_mx_dense("f32", 4, 64, x.data_ptr(), 1 << 33)):
         with pytest.raises(costa.CostaError) as e:
             costa.costa_mx_quantize(bad, "N", costa.costa_mx_matrix("e2m1", 4, 64, q.codes.data_ptr(),
