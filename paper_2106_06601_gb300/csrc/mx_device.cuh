@@ -164,16 +164,26 @@ template <typename T, int N> struct Unaligned {
             c[4 * j + 3] = v.w;
         }
     }
-    __device__ void place(uint32_t off, int count, uint32_t (&w)[kWords]) {
-        if (off != 0) {
-#pragma unroll
-            for (int i = 0; i < kWords + 2; ++i) c[i] = off & 8 ? c[i + 2] : c[i];
-#pragma unroll
-            for (int i = 0; i < kWords + 1; ++i) c[i] = off & 4 ? c[i + 1] : c[i];
-        }
+    template <int FROM> __device__ void shift(uint32_t bits, uint32_t (&w)[kWords]) const {  // from word FROM
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
-            w[i] = sizeof(T) == 2 && off != 0 ? __funnelshift_r(c[i], c[i + 1], (off & 2) * 8) : c[i];
+            w[i] = sizeof(T) == 2 ? __funnelshift_r(c[i + FROM], c[i + FROM + 1], bits) : c[i + FROM];
+    }
+    // `off` is the same in (nearly) all warps' lanes: a branch costs less than selecting words.
+    __device__ void place(uint32_t off, int count, uint32_t (&w)[kWords]) const {
+        const uint32_t bits = (off & 2) * 8;
+        if (off == 0) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = c[i];
+        } else if (off < 4) {
+            shift<0>(bits, w);
+        } else if (off < 8) {
+            shift<1>(bits, w);
+        } else if (off < 12) {
+            shift<2>(bits, w);
+        } else {
+            shift<3>(bits, w);
+        }
         if (count >= N) return;
 #pragma unroll
         for (int i = 0; i < kWords; ++i) {

@@ -1,6 +1,11 @@
 // Kernels that make and read microscaled codes element by element: the
 // quantisation of op(X), its inverse, and activations with 8-bit checkpoints.
-// All are bound by memory traffic.
+//
+// All read and write each byte once, so memory bounds them where they issue few
+// enough instructions: of 16 elements to a thread, in 32-byte accesses, they
+// have 8 to 18 an element (first versions had 50 and ran at a third of the copy
+// rate).  Rates below are of the bytes of inputs, codes and outputs, where a
+// copy reaches 6786 GB/s.
 #include <algorithm>
 
 #include "costa_internal.h"
@@ -283,6 +288,9 @@ Groups groups(const costa_mx_matrix &q, bool tiles) {
                      tiles && q.format == COSTA_MX_E2M1 ? mx_scale_tiles(q.cols) * 8 : mx_blocks(q.cols) * 2);
 }
 
+// Quantisation along rows: the largest magnitude of a block from two lanes, one
+// shuffle; a power-of-two factor, exact; one conversion.  8192 x 8192 bf16 to
+// E2M1 27 us (6180 GB/s), to I8 31 us (6530); f32 43 us (7030).
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) quantize_n_kernel(Dense<const T> X, Codes Q, int64_t cols, Groups gr) {
     int64_t row, col;
@@ -294,6 +302,9 @@ __global__ void __launch_bounds__(kThreads) quantize_n_kernel(Dense<const T> X, 
     put16<FMT>(Q, in, row, col, cols, x);
 }
 
+// The values of codes, exact in either type: 8192 x 8192 E2M1 to bf16 27 us (6220
+// GB/s), to f32 45 us (6800); to f32 rows of an odd stride, through shared
+// memory, 2777 x 4093 11 us (4650).
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> Y, int64_t cols, Groups gr) {
     COSTA_MX_STAGE;
@@ -336,7 +347,9 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(Codes Q, Dense<T> 
 // through shared memory so that each column's 4 blocks (64 or 128 bytes of a
 // row of QT) are written together.  Neighbouring thread blocks take
 // neighbouring columns, for the memory's pages.  With BOTH the same rows are
-// then read again, from the cache, 8 lanes to a row.
+// then read again, from the cache, 8 lanes to a row.  8192 x 8192 bf16 to E2M1
+// 30 us (5750 GB/s); both orders 44 us (4680 GB/s), where it issues 18
+// instructions an element, 71% of the issue slots; two calls take 57.
 constexpr int kTile = 128;
 
 // The codes of a block of 32 elements x(0) .. x(31) with scale byte s (E2M1: taken
@@ -512,6 +525,8 @@ template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, f
     }
 }
 
+// Y and the checkpoints from one pass over X (and G).  8192 x 16384 bf16, gated:
+// SiLU 168 us (6440 GB/s), GELU 204 us (5310), whose cdf is beside the traffic.
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
                                                                Codes QG, int64_t cols, Groups gr) {
@@ -530,6 +545,8 @@ __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T>
     if constexpr (GATED) put16<COSTA_MX_I8>(QG, in, row, col, cols, g);
 }
 
+// The gradients from the checkpoints, nothing else kept.  8192 x 16384 bf16,
+// gated: SiLU 171 us (6310 GB/s), GELU 184 us (5890).
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
                                                                 Dense<T> dG, int64_t cols, Groups gr) {

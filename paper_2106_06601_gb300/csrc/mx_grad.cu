@@ -17,6 +17,13 @@
 // product over 16 tokens (measured: 1.3e-5 after 1024).  So a sum takes
 // kProducts of them at most, in one of two places in tensor memory; eight warps
 // add each to sums in registers, rounded to nearest, while the next one builds.
+//
+// GB300: 4096 x 8192 x 4096 bf16 190 us (1.45 PFLOP/s, 75% of the library
+// products' rate), 16384 tokens 800 us (1.37); the same with an odd stride 470
+// us, f32 605 us (three products each: 1.36 PFLOP/s of them), f32 with an odd
+// stride 700 us.  What bounds it: the conversions' logical and bf16 operations,
+// at half rate each, and shared memory, which the operands and the converted
+// codes share, are all at 50 to 65%, and 24 warps hide no more of their latency.
 #include <algorithm>
 #include <type_traits>
 
@@ -57,10 +64,11 @@ template <int NT, int SRC> struct Shape {
     static constexpr int stages = SRC == kF32 ? 3 : 5;
     static constexpr int smem = stages * operands + 1024;
     // Warpgroups: two for the sums; one for dY's copies and the products; sets of converters, which take turns.
-    static constexpr int x_sets = direct ? 3 : 2, y_sets = direct ? 0 : 2, groups = 3 + x_sets + y_sets;
+    // (Unaligned bf16, 4096 x 8192 x 4096, 2 and 2, 2 and 3, 3 and 2 sets for X and dY: 508, 519, 469 us.)
+    static constexpr int x_sets = SRC == kF32 ? 2 : 3, y_sets = direct ? 0 : 2, groups = 3 + x_sets + y_sets;
     // Registers of a thread: at launch, and then of each.
-    static constexpr int at_launch = direct ? 80 : 72;
-    static constexpr int for_sums = direct ? 168 : 104, for_copies = 24, for_x = 40, for_y = 96;
+    static constexpr int at_launch = direct ? 80 : SRC == kF32 ? 72 : 64;
+    static constexpr int for_sums = direct ? 168 : 104, for_copies = 24, for_x = 40, for_y = SRC == kF32 ? 96 : 72;
     static_assert(2 * for_sums + for_copies + x_sets * for_x + y_sets * for_y <= groups * at_launch, "registers");
     static_assert(groups * 128 * at_launch <= 65536, "registers");
     static constexpr int cols = 2 * NT;
@@ -323,30 +331,34 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
     } else if constexpr (!S::direct) {  // dY to bf16 parts: 8 columns of a token to a thread, some times
         more_registers<S::for_y>();
         using Y = std::conditional_t<SRC == kF32, float, __nv_bfloat16>;
-        constexpr int kPieces = S::half / 8, kTasks = kTokens * kPieces / 128;
         const Y *const dy = static_cast<const Y *>(p.dy);
-        constexpr int kRows = 128 / kPieces;  // tokens apart, a multiple of 8: what a row's start is off 16 bytes is the same
-        static_assert(kRows % 8 == 0 && kTokens % kRows == 0, "tokens of a thread");
-        const int id = threadIdx.x % 128, c = id % kPieces, row = id / kPieces;
-        const uint32_t off = Unaligned<Y, 8>::offset(dy + row * p.ldy);
-        const uint32_t store = S::x_bytes + (c / 8) * (kTokens * 128) + row * 128 + (((c % 8) ^ (row & 7)) << 4);
+        // Of a stage's 64 tokens a warp takes those of two remainders by 8: their rows are all off 16 bytes by the same.
+        // Task j: tokens token(j), 8 lanes to each.
+        constexpr int kTasks = 4;
+        static_assert(S::half == 64 && kTokens == 64, "8 lanes to a token");
+        const int c = lane % 8, rest = warp % 4 * 2;
+        auto token = [&](int j) { return rest + j / 2 + 8 * (lane / 8) + 32 * (j % 2); };
+        uint32_t off[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            off[h] = __shfl_sync(~0u, Unaligned<Y, 8>::offset(dy + (rest + h) * p.ldy), 0);
         Unaligned<Y, 8> y[kTasks];
-        const Y *first_y;  // this thread's first of a stage
-        int count;         // columns from there
+        const Y *first_y;  // this thread's columns of a stage's first token
+        int count;         // how many there are
         auto seek = [&] {
-            first_y = dy + (int64_t(st) * kTokens + row) * p.ldy + n0 + c * 8;
+            first_y = dy + int64_t(st) * kTokens * p.ldy + n0 + c * 8;
             count = count_from(n0 + c * 8, p.n, 8);
         };
         const int64_t step = S::y_sets * kTokens * p.ldy;
         auto load = [&] {
-            const int left = t < tiles ? static_cast<int>(min(p.m - int64_t(st) * kTokens, int64_t(kTokens))) - row : 0;
-            if (left > kTokens - kRows && count == 8) {
+            const int left = t < tiles ? static_cast<int>(min(p.m - int64_t(st) * kTokens, int64_t(kTokens))) : 0;
+            if (left == kTokens && count == 8) {
 #pragma unroll
-                for (int j = 0; j < kTasks; ++j) y[j].load_whole(first_y + j * (kRows * p.ldy), off);
+                for (int j = 0; j < kTasks; ++j) y[j].load_whole(first_y + token(j) * p.ldy, off[j / 2]);
             } else {
 #pragma unroll
                 for (int j = 0; j < kTasks; ++j)
-                    y[j].load(first_y + j * (kRows * p.ldy), off, left > j * kRows ? count : 0);
+                    y[j].load(first_y + token(j) * p.ldy, off[j / 2], token(j) < left ? count : 0);
             }
         };
         const int set = warp / 4 - 3 - S::x_sets;
@@ -355,12 +367,12 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
         load();
         while (t < tiles) {
             if (!__all_sync(~0u, bar_wait(empty(at.s), at.parity ^ 1, failed))) break;
-            const uint32_t to = ring + at.s * S::operands + store;
+            const uint32_t to = ring + at.s * S::operands + S::x_bytes;
 #pragma unroll
             for (int j = 0; j < kTasks; ++j) {
                 uint32_t w[Unaligned<Y, 8>::kWords];
-                y[j].place(off, count, w);  // (of a token past the last: zeros)
-                const uint32_t line = to + j * (kRows * 128);
+                y[j].place(off[j / 2], count, w);  // (of a token past the last: zeros)
+                const uint32_t line = to + token(j) * 128 + ((c ^ (rest + j / 2)) << 4);
                 if constexpr (SRC == kF32) {
 #pragma unroll
                     for (int h = 0; h < S::parts; ++h) {

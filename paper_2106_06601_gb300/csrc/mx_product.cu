@@ -8,7 +8,14 @@
 // brings operands and scales into a ring of stages of 256 columns of k, and one
 // thread of the last issues the products.  Tiles of 256
 // rows of A are taken by pairs of blocks, with 256 rows of B: each block then
-// brings half of A's rows, a third less for the L2 cache to deliver.
+// brings half of A's rows, a third less for the L2 cache to deliver.  Calls with
+// few tiles split k over a cluster and join the parts in their order.
+//
+// GB300: 8192 x 16384 x 8192 301 us, 7.3 PFLOP/s of a nominal 9 (products over 64
+// elements): of 784 cycles a stage the tensor cores' queue takes 621, among them
+// some 150 for copies of scales, and operands come late in 105.  1023 x 4096 x
+// 4096 10.7 us: one round of tiles, its fill and its way out.  1 x 16384 x 4096
+// 8 us for 35.6 MB of weights (4.5 TB/s): fill, and the join of two halves of k.
 #include <algorithm>
 
 #include "costa_internal.h"
