@@ -66,7 +66,8 @@ template <int NT, int SRC> struct Shape {
     // Warpgroups: two for the sums; one for dY's copies and the products; sets of converters, which take turns.
     // (Unaligned bf16, 4096 x 8192 x 4096, 2 and 2, 2 and 3, 3 and 2 sets for X and dY: 508, 519, 469 us.)
     static constexpr int x_sets = SRC == kF32 ? 2 : 3, y_sets = direct ? 0 : 2, groups = 3 + x_sets + y_sets;
-    // Registers of a thread: at launch, and then of each.
+    // Registers of a thread: at launch, and then of each.  (Nothing here may call a function that is not inlined: its
+    // code would use registers that a warp has given up.)
     static constexpr int at_launch = direct ? 80 : SRC == kF32 ? 72 : 64;
     static constexpr int for_sums = direct ? 168 : 104, for_copies = 24, for_x = 40, for_y = SRC == kF32 ? 96 : 72;
     static_assert(2 * for_sums + for_copies + x_sets * for_x + y_sets * for_y <= groups * at_launch, "registers");

@@ -429,6 +429,35 @@ def test_streams_and_graph():
         check(X.view.double().cpu().numpy())
 
 
+def test_two_streams_at_once():
+    """Products of every tile size and gradients of every source on two streams, which share SMs and tensor memory."""
+    rng = np.random.default_rng(13)
+    work = []
+    for m, n, k in ((3, 900, 700), (30, 900, 700), (60, 2000, 500), (120, 900, 700), (700, 5000, 300)):
+        A, a = codes_of("e2m1", matrix(rng, m, k, "f32"))
+        B, b = codes_of("e2m1", matrix(rng, n, k, "f32"))
+        C = Dense(m, n, "f32")
+        work.append((lambda A=A, B=B, C=C: costa.costa_mx_product(A.c, B.c, C.c, stream=stream()),
+                     lambda C=C, a=a, b=b, k=k: check_product(C, a, b, None, 1.0, 0.0, "f32", k)))
+    for m, n, k, kind, pad in ((300, 200, 300, "bf16", 0), (300, 200, 300, "bf16", 1), (300, 200, 300, "f32", 0),
+                               (200, 2600, 2100, "bf16", 0)):
+        dy = matrix(rng, m, n, kind)
+        dY, dW = Dense(m, n, kind, dy, pad), Dense(n, k, "f32")
+        q, x = codes_of("i8", matrix(rng, m, k, "f32"))
+        work.append((lambda dY=dY, q=q, dW=dW: costa.costa_mx_weight_grad(dY.c, q.c, dW.c, stream=stream()),
+                     lambda dW=dW, dy=dy, x=x, m=m: check_product(dW, dy.T.astype(np.float64), x.T, None, 1.0, 0.0,
+                                                                  "f32", 3 * m)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(4):
+        for i, (call, _) in enumerate(work):  # a call stays on its stream; its neighbour runs beside it
+            with torch.cuda.stream(streams[i % 2]):
+                call()
+    torch.cuda.synchronize()
+    for _, check in work:
+        check()
+
+
 def test_storage_refusals():
     """Host memory and matrices that leave their allocation are refused before any kernel runs."""
     host = np.zeros(4096, np.uint8)
