@@ -55,8 +55,8 @@ template <typename T> __global__ void scale_kernel(T *c, int64_t ld, int64_t row
 }  // namespace
 
 cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint64_t rows, uint64_t pitch,
-                        uint32_t box_rows, bool swizzle) {
-    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, width, rows, pitch, 128, box_rows, swizzle);
+                        uint32_t box_rows) {
+    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, width, rows, pitch, 128, box_rows, true);
 }
 
 cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t ld,

@@ -45,10 +45,10 @@ cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, size_t 
 }
 
 // 2-D tensor maps, zeros outside, 128-byte swizzle: of bytes, `width` bytes x
-// `rows`, `pitch` bytes from row to row, in boxes of 128 bytes x `box_rows`
-// (swizzled or not); of bf16, in boxes of 64 elements.
+// `rows`, `pitch` bytes from row to row, in boxes of 128 bytes x `box_rows`; of
+// bf16, in boxes of 64 elements.
 cudaError_t mx_byte_map(CUtensorMap *map, const void *base, uint64_t width, uint64_t rows, uint64_t pitch,
-                        uint32_t box_rows, bool swizzle);
+                        uint32_t box_rows);
 cudaError_t mx_bf16_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t ld,
                         uint32_t box_rows);
 // Of tiles of scales (512 bytes), in boxes of `box_tiles`, not swizzled.

@@ -294,8 +294,8 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     using S = Shape<NT>;
     const int64_t nb = mx_blocks(A.cols);
     CUtensorMap a_map, b_map, a_scale_map, b_scale_map;
-    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, S::a_rows, true);
-    if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows, true);
+    cudaError_t e = mx_byte_map(&a_map, A.codes, 16 * nb, A.rows, A.ld, S::a_rows);
+    if (e == cudaSuccess) e = mx_byte_map(&b_map, B.codes, 16 * nb, B.rows, B.ld, kRows);
     if constexpr (S::pair) {
         const int64_t tiles_k = mx_scale_tiles(A.cols), a_tiles = mx_ceil(A.rows, 128) * tiles_k,
                       b_tiles = mx_ceil(B.rows, 128) * tiles_k;
