@@ -10,7 +10,9 @@
 namespace costa {
 namespace mx {
 
-// The first call of every kernel: from here on the next kernel's blocks may start.
+// From here on the next kernel's blocks may start.  The first call of every
+// kernel; in those that use tensor memory once they hold it: a kernel that waits
+// for this one must not hold what this one still waits for.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // Before anything in global memory is read or written: what the kernels before this one wrote is there.
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -132,7 +132,6 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = static_cast<int>(cluster_rank()), half = rank & 1, lead = rank & ~1, part = rank >> 1;
 
-    let_next_start();
     if (threadIdx.x == 0) {
         failed_word = 0;
         for (int s = 0; s < S::stages; ++s) {
@@ -151,6 +150,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
     cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
+    let_next_start();
     after_previous();
 
     // This block's share of the tokens, in stages; and its tiles.

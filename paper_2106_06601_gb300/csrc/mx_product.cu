@@ -88,7 +88,6 @@ __global__ void __launch_bounds__(Shape<NT>::threads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = static_cast<int>(cluster_rank()), half = kPair ? rank & 1 : 0;
 
-    let_next_start();
     if (threadIdx.x == 0) {
         failed_word = 0;
         for (int s = 0; s < S::stages; ++s) {
@@ -112,6 +111,7 @@ __global__ void __launch_bounds__(Shape<NT>::threads, 1)
     if constexpr (kPair) cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_slot;
+    let_next_start();
 
     // This block's share of k, in stages; and its tiles.  (Pairs do not split k.)
     const int stages_k = (p.steps + 3) / 4;
