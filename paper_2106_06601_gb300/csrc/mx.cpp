@@ -304,7 +304,8 @@ costa_status costa_mx_weight_grad(const costa_mx_dense *dY, const costa_mx_matri
 costa_status costa_mx_failures(int64_t *count) {
     if (!count) return bad(COSTA_ERR_INVALID_ARG, "count is null");
     unsigned a = 0, b = 0;
-    cudaError_t e = mx_product_failures(&a);
+    cudaError_t e = cudaDeviceSynchronize();  // the copies alone would not wait for non-blocking streams
+    if (e == cudaSuccess) e = mx_product_failures(&a);
     if (e == cudaSuccess) e = mx_grad_failures(&b);
     if (e != cudaSuccess) return done(e, "costa_mx_failures");
     *count = int64_t(a) + b;

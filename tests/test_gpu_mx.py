@@ -458,6 +458,23 @@ def test_two_streams_at_once():
         check()
 
 
+def test_failures_waits_for_all_streams():
+    """The count is that of all calls so far, those on non-blocking streams too."""
+    A, B = (Codes("e2m1", 4096, 4096) for _ in range(2))
+    for q in (A, B):
+        q.codes.zero_()
+        q.scales.zero_()
+    C = torch.empty(4096, 4096, device="cuda")
+    c = costa.costa_mx_dense("f32", 4096, 4096, C.data_ptr(), 4096)
+    assert costa.costa_mx_failures() == 0  # (a first call may wait for other reasons)
+    side, done = torch.cuda.Stream(), torch.cuda.Event()
+    for _ in range(200):  # some 10 ms
+        costa.costa_mx_product(A.c, B.c, c, stream=side.cuda_stream)
+    done.record(side)
+    assert costa.costa_mx_failures() == 0
+    assert done.query()
+
+
 def test_storage_refusals():
     """Host memory and matrices that leave their allocation are refused before any kernel runs."""
     host = np.zeros(4096, np.uint8)
