@@ -659,6 +659,9 @@ costa_status costa_phase_times(double *ms, int *nphases);
  *    (COSTA_ERR_LAYOUT).  Dense inputs whose rows are not 16-byte aligned may
  *    be read in whole aligned 16-byte chunks, as costa_block's source runs.
  *    Outputs are written element by element; nothing outside them is.
+ *  - Overlap: outputs overlap neither inputs nor each other, except that an
+ *    activation's Y may be X or G, and dX or dG may be dY (the same pointer and
+ *    ld).  Other overlap is not detected and gives undefined contents.
  *  - Kernels start as programmatic dependents of the kernel before them on the
  *    stream; they read and write nothing until it is complete. */
 

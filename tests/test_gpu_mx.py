@@ -255,6 +255,32 @@ def test_act(rows, cols, name, dtype, gated, pad):
         close(dG.numpy(), dy * back, np.abs(dy) * unit * np.abs(xr) + 2 * EPS[dtype] * np.abs(dy * back) + 1e-38)
 
 
+@pytest.mark.parametrize("rows, cols", ACT_SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3, 8])
+@pytest.mark.parametrize("over", ["first", "second"])
+def test_act_in_place(rows, cols, dtype, pad, over):
+    """Y over X or G, dX or dG over dY: the same bits, checkpoints too, as with storage of their own."""
+    rng = np.random.default_rng([rows, cols, pad])
+    x, g, dy = (matrix(rng, rows, cols, dtype) for _ in range(3))
+    dense = lambda v=None: Dense(rows, cols, dtype, v, pad, pad)
+
+    def run(in_place):
+        X, G, dY = dense(x), dense(g), dense(dy)
+        Y = dense() if not in_place else X if over == "first" else G
+        dX = dY if in_place and over == "first" else dense()
+        dG = dY if in_place and over == "second" else dense()
+        qx, qg = Codes("i8", rows, cols), Codes("i8", rows, cols)
+        costa.costa_mx_act_forward("silu", X.c, G.c, Y.c, qx.c, qg.c, stream())
+        costa.costa_mx_act_backward("silu", qx.c, qg.c, dY.c, dX.c, dG.c, stream())
+        qx.check(x)
+        qg.check(g)
+        return [v.numpy() for v in (Y, dX, dG)]
+
+    for got, want in zip(run(True), run(False)):
+        assert np.array_equal(got, want)
+
+
 @pytest.mark.parametrize("name", ["silu", "gelu"])
 def test_act_gradient_against_differences(name):
     """Central differences of the forward pass at the checkpoint's values, in 64 bits on the definition's side and
