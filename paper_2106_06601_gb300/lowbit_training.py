@@ -138,7 +138,7 @@ def run(steps: int = 20, tokens: int = 512, width: int = 256, hidden: int = 768,
         y, kept = layer.forward(x)
         off = y.float() - target
         losses.append(off.square().mean().div(2))
-        layer.backward((off / tokens).bfloat16(), kept)
+        layer.backward((off / tokens).bfloat16(), kept)  # of the mean over tokens of the sum over columns
         layer.update(lr)
     return [float(v) for v in losses]
 
