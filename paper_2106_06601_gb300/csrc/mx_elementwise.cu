@@ -153,7 +153,9 @@ __device__ __forceinline__ void get(const Dense<const T> &X, int64_t row, int64_
 // The elements of a warp's 32 groups on their way to rows that are not aligned
 // or end inside a group: the lanes write a block's 32 elements together, from 2
 // KB of shared memory of the warp.  Lane 2 i holds block i's place and how many
-// of its elements exist; in most warps all blocks follow each other in a row.
+// of its elements exist; in most warps the blocks are one run in memory: they
+// follow each other, and each but the last with elements is whole.  (Where rows
+// are apart by whole blocks the next row also follows a block that is cut short.)
 struct Blocks {
     int64_t place, first;
     int count, left;
@@ -162,7 +164,8 @@ struct Blocks {
         : place(row * ld + col), count(count_from(col, cols, 32)) {
         const int lane = threadIdx.x % 32;
         first = __shfl_sync(~0u, place, 0);
-        run = __all_sync(~0u, place == first + 16 * lane || count == 0);
+        const uint32_t some = __ballot_sync(~0u, lane % 2 == 0 && count > 0), cut = __ballot_sync(~0u, count < 32);
+        run = __all_sync(~0u, place == first + 16 * lane || count == 0) && (some & cut << 2) == 0;
         // elements from the first on: whole blocks, then one that may end, then none
         left = __reduce_add_sync(~0u, lane % 2 ? 0 : count);
     }

@@ -281,6 +281,58 @@ def test_act_in_place(rows, cols, dtype, pad, over):
         assert np.array_equal(got, want)
 
 
+# Rows that are whole blocks apart (the usual rounding up of a stride), so that a row's first block follows the cut one
+# of the row before it as if they were one run; 32 more; and 16, where rows are whole groups apart.
+ROW_ENDS = [(2, 13), (16, 13), (31, 31), (64, 33), (20, 40), (33, 48), (64, 90), (16, 257), (70, 300), (9, 480), (5, 4099),
+            (64, 2777)]
+
+
+def apart(cols, more):
+    return -cols % (16 if more == "groups" else 32) + (32 if more == "more" else 0)
+
+
+@pytest.mark.parametrize("rows, cols", ROW_ENDS)
+@pytest.mark.parametrize("fmt", ["e2m1", "i8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("more", ["blocks", "more", "groups"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_dequantize_rows_whole_blocks_apart(rows, cols, fmt, dtype, more, shift):
+    x = matrix(np.random.default_rng([rows, cols]), rows, cols, "bf16")  # whose codes' values are exact in either type
+    q, want = codes_of(fmt, x)
+    Y = Dense(rows, cols, dtype, None, apart(cols, more), shift)
+    costa.costa_mx_dequantize(q.c, Y.c, stream())
+    assert np.array_equal(Y.numpy(), want)
+
+
+@pytest.mark.parametrize("rows, cols", ROW_ENDS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("more", ["blocks", "more", "groups"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_act_rows_whole_blocks_apart(rows, cols, dtype, gated, more, shift):
+    """The same bits as in rows without gaps, guards around them, in storage of their own and in place."""
+    rng = np.random.default_rng([rows, cols])
+    x, g, dy = (matrix(rng, rows, cols, dtype) for _ in range(3))
+
+    def run(pad, shift, in_place):
+        dense = lambda v=None: Dense(rows, cols, dtype, v, pad, shift)
+        X, dY, qx = dense(x), dense(dy), Codes("i8", rows, cols)
+        Y, dX = (X, dY) if in_place else (dense(), dense())
+        G, dG, qg = (dense(g), dense(), Codes("i8", rows, cols)) if gated else (None, None, None)
+        c = lambda v: v.c if v is not None else None
+        costa.costa_mx_act_forward("silu", X.c, c(G), Y.c, qx.c, c(qg), stream())
+        costa.costa_mx_act_backward("silu", qx.c, c(qg), dY.c, dX.c, c(dG), stream())
+        qx.check(x)
+        if gated:
+            qg.check(g)
+        return [v.numpy() for v in (Y, dX, dG) if v is not None]
+
+    want = run(0, 0, False)
+    for in_place in (False, True):
+        for got, w in zip(run(apart(cols, more), shift, in_place), want):
+            assert np.array_equal(got, w)
+
+
 @pytest.mark.parametrize("name", ["silu", "gelu"])
 def test_act_gradient_against_differences(name):
     """Central differences of the forward pass at the checkpoint's values, in 64 bits on the definition's side and
