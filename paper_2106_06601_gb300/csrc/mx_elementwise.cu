@@ -497,56 +497,99 @@ __global__ void __launch_bounds__(kThreads, 4) quantize_t_kernel(Dense<const T> 
     }
 }
 
-// 1 / (1 + e^-x) within 2^-22 + |x| 2^-23 of itself: nothing beside |x| 2^-20,
-// the unit of what uses it.  Beyond the range of e^-x it is 0 or 1.
-__device__ __forceinline__ float sigmoid(float x) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+// SiLU and GELU are accurate to their own size, in the tails too.  f32: within 10
+// and 19 units of 2^-24 of themselves, down to where e^-|x| or e^(-x^2 / 2) is
+// subnormal.  bf16, whose rounding is off by up to 2^-8: within 2^-16 and 2^-15,
+// with cheaper exponentials (8192 x 16384 gated, the f32 forms: SiLU forward 197
+// us for 181, GELU 235 and backward 212 for 203 and 174); they flush to 0 what
+// is below 2^-126, where the result is below |x| 2^-126.
+template <typename T> constexpr bool kShort = sizeof(T) == 2;
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
+}
+__device__ __forceinline__ float fast_inverse(float x) {  // of x >= 1
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
-// The normal distribution's cdf at x, and e^(-x^2 / 2): Abramowitz and Stegun's
-// 7.1.26, five terms in t = 1 / (1 + p |x| / sqrt(2)), within 0.75e-7.
-__device__ __forceinline__ float normal_cdf(float x, float &e) {
-    float t;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(fabsf(x), 0.3275911f * 0.7071067811865476f, 1.0f)));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * x * (-0.5f * 1.4426950408889634f)));
-    float s = fmaf(t, 1.061405429f, -1.453152027f);
-    s = fmaf(t, s, 1.421413741f);
-    s = fmaf(t, s, -0.284496736f);
-    s = fmaf(t, s, 0.254829592f);
-    const float tail = 0.5f * t * s * e;
+// s = 1 / (1 + e^-x) and rest = 1 - s; f32: both from e^-|x| <= 1, so that neither is a difference.
+template <typename T> __device__ __forceinline__ float sigmoid(float x, float &rest) {
+    if constexpr (kShort<T>) {
+        const float s = fast_inverse(1.0f + fast_exp2(x * -1.4426950408889634f));
+        rest = 1.0f - s;
+        return s;
+    } else {
+        const float e = expf(-fabsf(x)), r = fast_inverse(1.0f + e), t = e * r;
+        rest = x < 0.0f ? r : t;
+        return x < 0.0f ? t : r;
+    }
+}
+
+// The normal distribution's cdf at x, and e^(-x^2 / 2).  The tail beyond |x| is
+// e^(-x^2 / 2) R(|x|); R falls slowly.  With t = 1 / (1 + p |x|), R / t is taken as
+// a polynomial, in u = 1 - t from 1/2 at 0 (f32) or in t (bf16), fitted for the
+// least relative error: 3.6e-8 on 0 .. 14.5, past which the tail is below 2^-149,
+// and 4.7e-6 on 0 .. 13.2.  f32 takes x^2 with what its rounding leaves.
+template <typename T> __device__ __forceinline__ float normal_cdf(float x, float &e) {
+    float tail;
+    if constexpr (kShort<T>) {
+        const float t = fast_inverse(fmaf(fabsf(x), 0.31f, 1.0f));
+        float s = fmaf(t, -0.0739290646f, 0.180450087f);
+        s = fmaf(t, s, 0.0157450492f);
+        s = fmaf(t, s, 0.133429573f);
+        s = fmaf(t, s, 0.120441339f);
+        s = fmaf(t, s, 0.123860695f);
+        e = fast_exp2(x * x * (-0.5f * 1.4426950408889634f));
+        tail = t * s * e;
+    } else {
+        const float a = fminf(fabsf(x), 16.0f), t = fast_inverse(fmaf(a, 0.35f, 1.0f)), u = 1.0f - t;
+        float s = fmaf(u, -0.0289184507f, 0.0883767232f);
+        s = fmaf(u, s, -0.0627829507f);
+        s = fmaf(u, s, -0.0170807354f);
+        s = fmaf(u, s, -0.0637271628f);
+        s = fmaf(u, s, 0.102527089f);
+        s = fmaf(u, s, 0.261060268f);
+        s = fmaf(u, s, -0.639832914f);
+        s = fmaf(u, s, 0.5f);
+        const float square = a * a, left = fmaf(a, a, -square);
+        e = expf(-0.5f * square);
+        e = fmaf(e, -0.5f * left, e);
+        tail = t * s * e;
+    }
     return x < 0.0f ? tail : 1.0f - tail;
 }
 
-// act(x) and act'(x).
-template <int ACT> __device__ __forceinline__ float act(float x) {
-    if constexpr (ACT == COSTA_MX_SILU) return x * sigmoid(x);
-    if constexpr (ACT == COSTA_MX_GELU) {
-        float e;
-        return x * normal_cdf(x, e);
-    }
+// act(x) and act'(x), for results of type T.
+template <int ACT, typename T> __device__ __forceinline__ float act(float x) {
+    float unused;
+    if constexpr (ACT == COSTA_MX_SILU) return x * sigmoid<T>(x, unused);
+    if constexpr (ACT == COSTA_MX_GELU) return x * normal_cdf<T>(x, unused);
     return x > 0.0f || x != x ? x : 0.0f;
 }
-template <int ACT> __device__ __forceinline__ void act_both(float x, float &y, float &slope) {
+template <int ACT, typename T> __device__ __forceinline__ void act_both(float x, float &y, float &slope) {
     if constexpr (ACT == COSTA_MX_SILU) {
-        const float s = sigmoid(x);
+        float rest;
+        const float s = sigmoid<T>(x, rest);
         y = x * s;
-        slope = s * (1.0f + x * (1.0f - s));
+        slope = kShort<T> ? s * (1.0f + x * rest) : fmaf(y, rest, s);
     } else if constexpr (ACT == COSTA_MX_GELU) {
         float e;
-        const float c = normal_cdf(x, e);
+        const float c = normal_cdf<T>(x, e);
         y = x * c;
         slope = fmaf(x * e, 0.3989422804014327f, c);
     } else {
-        y = act<ACT>(x);
+        y = act<ACT, T>(x);
         slope = x != x ? x : x > 0.0f ? 1.0f : 0.0f;
     }
 }
 
-// Y and the checkpoints from one pass over X (and G).  8192 x 16384 bf16, gated:
-// SiLU 168 us (6440 GB/s), GELU 204 us (5310), whose cdf is beside the traffic.
+// Y and the checkpoints from one pass over X (and G).  8192 x 16384, gated, bf16:
+// SiLU 181 us (5980 GB/s), GELU 203 us (5330), whose cdf is beside the traffic; f32:
+// 266 us (7130) and 276 us (6890).
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
                                                                Codes QG, int64_t cols, Groups gr) {
@@ -559,14 +602,15 @@ __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T>
     get(X, row, col, cols, x);
     if constexpr (GATED) get(G, row, col, cols, g);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) y.set(i, GATED ? act<ACT>(x(i)) * g(i) : act<ACT>(x(i)));
+    for (int i = 0; i < 16; ++i) y.set(i, GATED ? act<ACT, T>(x(i)) * g(i) : act<ACT, T>(x(i)));
     put(Y, row, col, cols, stage, y);
     put16<COSTA_MX_I8>(QX, in, row, col, cols, x);
     if constexpr (GATED) put16<COSTA_MX_I8>(QG, in, row, col, cols, g);
 }
 
-// The gradients from the checkpoints, nothing else kept.  8192 x 16384 bf16,
-// gated: SiLU 163 us (6640 GB/s; with five blocks of an SM 171), GELU 174 us (6210).
+// The gradients from the checkpoints, nothing else kept.  8192 x 16384, gated, bf16:
+// SiLU 163 us (6640 GB/s; with five blocks of an SM 171), GELU 174 us (6220); f32:
+// 272 us (6990) and 280 us (6770).
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
                                                                 Dense<T> dG, int64_t cols, Groups gr) {
@@ -591,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) act_backward
         for (int j = 0; j < 4; ++j) {
             const int k = 4 * i + j;
             float y, slope;
-            act_both<ACT>(xs[j], y, slope);
+            act_both<ACT, T>(xs[j], y, slope);
             if constexpr (GATED) {
                 dg.set(k, d(k) * y);
                 dx.set(k, d(k) * gs[j] * slope);

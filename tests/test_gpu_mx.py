@@ -1,6 +1,8 @@
 """Low-bit matrices on the GPU against their definitions in 64 bits: codes and
 scales bit for bit; products, activations and gradients within bounds that
 follow from 32-bit sums and one rounding; nothing written outside the outputs."""
+import math
+
 import numpy as np
 import pytest
 
@@ -331,6 +333,67 @@ def test_act_rows_whole_blocks_apart(rows, cols, dtype, gated, more, shift):
     for in_place in (False, True):
         for got, w in zip(run(apart(cols, more), shift, in_place), want):
             assert np.array_equal(got, w)
+
+
+def act_terms(name, x):
+    """act(x), its slope, and the slope's terms' magnitudes, each accurate to its own size in the tails too."""
+    x = x.astype(np.float64)
+    if name == "silu":
+        e = np.exp(-np.abs(x))
+        s, c = np.where(x < 0, e, 1.0) / (1 + e), np.where(x < 0, 1.0, e) / (1 + e)
+        return x * s, s + x * s * c, s + np.abs(x) * s * c
+    cdf = 0.5 * np.vectorize(math.erfc, otypes=[float])(-x / math.sqrt(2))
+    density = np.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+    return x * cdf, cdf + x * density, cdf + np.abs(x) * density
+
+
+def act_points(rng):
+    """Both tails to where the functions underflow, the middle, and arguments down to the smallest."""
+    tails = np.linspace(-100, 100, 4001), np.linspace(-14, 14, 4001), rng.uniform(-2, 2, 4001)
+    small = np.exp2(-np.arange(0, 149.0))
+    x = np.concatenate([*tails, small, -small])
+    return np.resize(x, (96, 128)).astype(np.float32)
+
+
+# The errors in units of 2^-24 of the value.  f32: SiLU: e^-|x| 4 (the library's 2 units in the last place), 1 + e^-|x| 1
+# more, its reciprocal 2, two products 2.  GELU: the polynomial's argument 3, of which 2.3 times reach the value, its sum
+# 4, the fit 1, two products 2, e^(-x^2 / 2) 5.  A gate's product 1.  So 10 and 19 with all of them; slopes have two such
+# terms and a sum.  Where e^-|x| or e^(-x^2 / 2) is subnormal it is off by up to 2^-148.
+# bf16: the argument of the exponential, |x| or x^2 / 2, below 88 is rounded by 1.5 or 2.5 units of itself, the GELU's fit
+# is 79 units off: 2^8 and 2^9 with the rest.  What is below 2^-126 may be 0.
+ACT_UNITS = {"f32": {"silu": 10, "gelu": 19}, "bf16": {"silu": 256, "gelu": 512}}
+FLUSH = {"f32": 2.0 ** -148, "bf16": 2.0 ** -126}
+
+
+def check_act(got, want, tol, dtype):
+    """One rounding to the output's type, half a unit in its last place or of its least number, after `tol`."""
+    half, least = (2.0 ** -24, 2.0 ** -150) if dtype == "f32" else (2.0 ** -8, 2.0 ** -134)
+    close(got, want, tol + half * (np.abs(want) + tol) + least)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_act_is_accurate_in_the_tails(name, dtype):
+    """Y to its own size, not to that of X."""
+    x = act_points(np.random.default_rng(21))
+    x = _mx.bf16(x) if dtype == "bf16" else x
+    X, Y, q = Dense(*x.shape, dtype, x), Dense(*x.shape, dtype), Codes("i8", *x.shape)
+    costa.costa_mx_act_forward(name, X.c, None, Y.c, q.c, None, stream())
+    want = act_terms(name, x)[0]
+    check_act(Y.numpy(), want, ACT_UNITS[dtype][name] * 2.0 ** -24 * np.abs(want) + np.abs(x) * FLUSH[dtype], dtype)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_act_gradient_is_accurate_in_the_tails(name, dtype):
+    x = act_points(np.random.default_rng(22))
+    x[np.abs(x) > (80 if name == "silu" else 12.5)] = 0  # (slopes below 2^-110)
+    x = np.sort(x.reshape(-1)).reshape(x.shape)  # like with like: a block's step is 2^-7 of its largest
+    qx, xr = codes_of("i8", x)
+    dX = Dense(*x.shape, dtype)
+    costa.costa_mx_act_backward(name, qx.c, None, Dense(*x.shape, dtype, np.ones(x.shape)).c, dX.c, None, stream())
+    _, want, terms = act_terms(name, xr)
+    check_act(dX.numpy(), want, (2 * ACT_UNITS[dtype][name] + 2) * 2.0 ** -24 * terms, dtype)
 
 
 @pytest.mark.parametrize("name", ["silu", "gelu"])
