@@ -3,8 +3,8 @@
 //
 // A checkpoint's value is an integer below 2^7 times a power of two: exact in
 // bf16.  An f32 gradient is cut into three bf16 parts of 8 bits each (by
-// truncation, so no part overflows), and their products are summed in the same
-// accumulator.  So every product is that of the values, and only the sums round.
+// truncation, so no part overflows), all of which are multiplied.  So every
+// product is that of the values, and only the sums round.
 //
 // A pair of thread blocks takes a tile of 256 columns of X (the lanes of tensor
 // memory, 128 in each block: neighbouring elements of a row of dW) and NT
@@ -13,10 +13,16 @@
 // cores' layout.  dY comes by bulk copies as it is where it is bf16 with 16-byte
 // aligned rows (kDirect); else more warps load, cut and store it.
 //
-// The tensor cores' sums truncate, about 1.3e-8 of the sum's magnitude for each
-// product over 16 tokens (measured: 1.3e-5 after 1024).  So a sum takes
-// kProducts of them at most, in one of two places in tensor memory; eight warps
-// add each to sums in registers, rounded to nearest, while the next one builds.
+// The tensor cores' sums truncate: of each term what lies below some 2^-25 of the
+// largest.  For values of one sign that is about 1.3e-8 of the sum for each product
+// over 16 tokens (1.3e-5 after 1024).  So a sum takes kProducts of them at most, in
+// one of two places in tensor memory; eight warps add each to sums in registers,
+// rounded to nearest, while the next one builds.  An f32 gradient's second and third
+// parts have a sum of their own: beside the first parts' their 16 bits were cut off,
+// term by term (errors 2.2e-6 of the sum at any number of tokens, now 4e-8; 777 x
+// 1000 x 1531 15.2 -> 15.6 us, 4096 x 8192 x 4096 632 -> 622).  Values of one sign
+// whose magnitudes spread over 2^8 and 2^24: 4e-7 and 1.8e-6 in bf16, 1.3e-7 and
+// 8e-7 in f32.
 //
 // GB300: 4096 x 8192 x 4096 bf16 190 us (1.45 PFLOP/s, 75% of the library
 // products' rate), 16384 tokens 800 us (1.37); the same with an odd stride 470
@@ -72,8 +78,9 @@ template <int NT, int SRC> struct Shape {
     static constexpr int for_sums = direct ? 168 : 104, for_copies = 24, for_x = 40, for_y = SRC == kF32 ? 96 : 72;
     static_assert(2 * for_sums + for_copies + x_sets * for_x + y_sets * for_y <= groups * at_launch, "registers");
     static_assert(groups * 128 * at_launch <= 65536, "registers");
-    static constexpr int cols = 2 * NT;
-    static constexpr int chunk = kProducts / (parts * (kTokens / 16));  // stages to a sum
+    // f32: the first parts' products to one sum, the others' to another.
+    static constexpr int sums = SRC == kF32 ? 2 : 1, cols = 2 * NT * sums;
+    static constexpr int chunk = kProducts / (std::max(1, parts - 1) * (kTokens / 16));  // stages to a sum
     static_assert(smem <= 226 * 1024 && kCols * NT * 4 <= stages * operands, "shared memory");
 };
 
@@ -193,13 +200,24 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
             for (int c = 0; c < chunks && ok; ++c, sum.next()) {
                 ok = __all_sync(~0u, bar_wait(sum_full(sum.s), sum.parity, failed));
                 fence_after();
+                const uint32_t place = from + S::sums * sum.s * NT;
 #pragma unroll
                 for (int g = 0; g < S::half / 16; ++g) {
                     uint32_t r[16];
-                    tmem_ld16(from + sum.s * NT + g * 16, r);
-                    tmem_wait_ld(r);
+                    if constexpr (S::sums == 2) {
+                        uint32_t q[16];
+                        tmem_ld16(place + NT + g * 16, q);
+                        tmem_ld16(place + g * 16, r);
+                        tmem_wait_ld(q);
+                        tmem_wait_ld(r);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[g * 16 + i] += __uint_as_float(r[i]);
+                        for (int i = 0; i < 16; ++i) acc[g * 16 + i] += __uint_as_float(r[i]) + __uint_as_float(q[i]);
+                    } else {
+                        tmem_ld16(place + g * 16, r);
+                        tmem_wait_ld(r);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[g * 16 + i] += __uint_as_float(r[i]);
+                    }
                 }
                 fence_before();
                 __syncwarp();
@@ -248,7 +266,7 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
                         if (in_sum == 0 && !bar_wait(sum_empty(sum.s), sum.parity ^ 1, failed)) break;
                         if (!bar_wait(full(at.s), at.parity, failed)) break;
                         fence_after();
-                        const uint32_t d = tmem + sum.s * NT, from = ring + at.s * S::operands;
+                        const uint32_t d = tmem + S::sums * sum.s * NT, from = ring + at.s * S::operands;
                         // 64 columns to a group of kTokens rows of 128 bytes
                         const uint64_t dx = operand_desc(from, kTokens * 128, 1024);
 #pragma unroll
@@ -256,8 +274,8 @@ __global__ void __launch_bounds__(Shape<NT, SRC>::groups * 128, 1)
                             const uint64_t dy = operand_desc(from + S::x_bytes + h * S::y_part, kTokens * 128, 1024);
 #pragma unroll
                             for (int q = 0; q < kTokens / 16; ++q)
-                                mma_bf16_pair(d, dx + 128 * q, dy + 128 * q, idesc_bf16_pair(NT),
-                                              in_sum > 0 || h > 0 || q > 0);
+                                mma_bf16_pair(d + (h > 0 ? NT : 0), dx + 128 * q, dy + 128 * q, idesc_bf16_pair(NT),
+                                              in_sum > 0 || h > 1 || q > 0);
                         }
                         mma_commit_pair(empty(at.s), both);
                         if (++in_sum == S::chunk || st == s_last - 1) {

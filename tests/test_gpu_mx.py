@@ -453,6 +453,41 @@ def test_weight_grad(m, n, k, ytype, wtype, alpha, beta, pad, qpad):
                   3 * m)
 
 
+@pytest.mark.parametrize("m, n, k", [(64, 40, 70), (500, 130, 260), (2048, 130, 260), (2048, 1500, 1000)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_weight_grad_f32_sums_of_one_sign(m, n, k, pad):
+    """Full 24-bit gradients, values in 1 .. 2: products of the first 8 bits are multiples of 2^-13 below 4, of which 256
+    sum exactly; the others' sums are 2^-7 of those, of whose 17 terms each of 32 products cuts below 2^-24: 2.2 units of
+    2^-24 on average over the growing sum.  Then one rounding of either sum's total, one for each 256 tokens (half a unit
+    of a sum that grows: 8 at most of 2048), and up to 3 where parts of the tokens are joined."""
+    rng = np.random.default_rng([m, n])
+    dy = (1 + rng.random((m, n))).astype(np.float32)
+    q, x = codes_of("i8", rng.uniform(1, 1.98, (m, k)).astype(np.float32))
+    dW = Dense(n, k, "f32")
+    costa.costa_mx_weight_grad(Dense(m, n, "f32", dy, pad).c, q.c, dW.c, stream=stream())
+    want = dy.T.astype(np.float64) @ x
+    close(dW.numpy(), want, (2.2 + 1 + min(8, m / 512) + 3) * 2.0 ** -24 * want)
+
+
+@pytest.mark.parametrize("m, n, k", [(1000, 130, 260), (65536, 130, 260), (32768, 520, 1030)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_weight_grad_bf16_sums_of_one_sign(m, n, k, pad):
+    """A sum of 32 products over 16 tokens cuts 17 terms of each below 2^-24 of the growing sum (280 units of 2^-24), and
+    each 512 tokens are joined with one rounding: far below 17 m / 32 units of one long sum."""
+    rng = np.random.default_rng([m, n])
+    size = lambda: np.exp2(-rng.integers(0, 4, (m, 1)))
+    dy = _mx.bf16(((1 + rng.random((m, n))) * size()).astype(np.float32))
+    x = torch.from_numpy(((1 + rng.random((m, k))) * size()).astype(np.float32)).to("cuda")
+    q, xr = Codes("i8", m, k), torch.empty(m, k, device="cuda")
+    as_dense = lambda a: costa.costa_mx_dense("f32", m, k, a.data_ptr(), k)
+    costa.costa_mx_quantize(as_dense(x), "N", q.c, stream())
+    costa.costa_mx_dequantize(q.c, as_dense(xr), stream())
+    dY, dW = Dense(m, n, "bf16", dy, pad), Dense(n, k, "f32")
+    costa.costa_mx_weight_grad(dY.c, q.c, dW.c, stream=stream())
+    want = dy.T.astype(np.float64) @ xr.double().cpu().numpy()
+    close(dW.numpy(), want, (280 + m / 1024 + 3) * 2.0 ** -24 * want)
+
+
 def test_weight_grad_without_tokens():
     w = np.arange(12, dtype=np.float32).reshape(3, 4)
     dW, q = Dense(3, 4, "f32", w), Codes("i8", 0, 4)
