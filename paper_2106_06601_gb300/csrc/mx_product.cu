@@ -9,7 +9,8 @@
 // thread of the last issues the products.  Tiles of 256
 // rows of A are taken by pairs of blocks, with 256 rows of B: each block then
 // brings half of A's rows, a third less for the L2 cache to deliver.  Calls with
-// few tiles split k over a cluster and join the parts in their order.
+// few tiles split k over a cluster and join the parts in their order.  A long k
+// takes several sums of a tile, one after another.
 //
 // GB300: 8192 x 16384 x 8192 301 us, 7.3 PFLOP/s of a nominal 9 (products over 64
 // elements): of 784 cycles a stage the tensor cores' queue takes 621, among them
@@ -29,12 +30,16 @@ constexpr int kRows = 128;  // rows of B in a block's tile
 constexpr int kPrefetch = 4;  // stages of B on their way to the L2 early (0, 4, 8, 16: 1 x 16384 x 4096 10.5, 9.8, 10.1, 10.1 us)
 constexpr int kMaxSplit = 8;
 // A stage holds 256 elements of k: 128 bytes of a row, 2 tiles of scales.
+// The tensor cores' sums truncate: for values of one sign some 1.4e-8 of the sum for each product over 64 elements
+// (1.4e-5 after 65536 elements). So a sum in tensor memory takes 32 stages at most (8e-7 of it), and sums of a longer k
+// are joined in registers, rounded to nearest (LONG): 8192 x 8192 x 8448 163 -> 171 us, 4096 x 8192 x 32768 296 -> 307.
+// (16 stages: 3e-7, but 8192 x 16384 x 8192 302 -> 317 us, and 178, 320.)
+constexpr int kSumStages = 32;
 
 __device__ unsigned g_failed;
 
 struct Params {
     const uint8_t *a_scales, *b_scales;  // not for pairs
-    int64_t m;           // rows of A
     int steps;           // products of 64 elements over k
     int scale_tiles;     // tiles of scales over k
     int n_tiles, m_tiles;
@@ -65,8 +70,9 @@ template <int NT> struct Shape {
     static_assert(smem <= 226 * 1024 && kRows * NT * 4 <= stages * stage, "a tile's partial sums fit the stages");
 };
 
-template <int NT, typename T>
-__global__ void __launch_bounds__(Shape<NT>::threads, 1)
+// LONG: a block's k takes more than one sum.
+template <int NT, bool LONG, typename T>
+__global__ void __launch_bounds__(Shape<NT>::threads, LONG && NT <= 64 ? 2 : 1)
     product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                    const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap b_scale_map,
                    const Params p, const Output<T> out, const int split) {
@@ -118,6 +124,7 @@ __global__ void __launch_bounds__(Shape<NT>::threads, 1)
     const int part = kPair ? 0 : rank, per_tile = kPair ? 2 : split;
     const int k_first = static_cast<int>(int64_t(stages_k) * part / split);
     const int k_last = static_cast<int>(int64_t(stages_k) * (part + 1) / split);
+    const int sums = (k_last - k_first + kSumStages - 1) / kSumStages, sum_k = (k_last - k_first + sums - 1) / sums;  // LONG: stages of each
     const int tiles = p.n_tiles * p.m_tiles, first = blockIdx.x / per_tile, stride = gridDim.x / per_tile;
     // Few rows of A: the time is that of reading B, which starts while the kernel before this one ends.
     if (NT <= 64 && warp == S::writers && first < tiles && elect_one())
@@ -171,12 +178,12 @@ __global__ void __launch_bounds__(Shape<NT>::threads, 1)
             Ring<S::stages> at;
             int done = 0;
             uint32_t turn = 0;
-            for (int t = first; t < tiles && !*failed; t += stride, ++done) {
+            for (int t = first, from_k = k_first; t < tiles && !*failed; ++done) {  // all sums of this block's tiles
                 const uint32_t d = tmem + (done & 1 ? S::second : 0);
-                const int before = done - kLag;
+                const int before = done - kLag, to_k = LONG ? min(k_last, from_k + sum_k) : k_last;
                 if (before >= 0 && !bar_wait(sum_empty(before & 1), (before >> 1) & 1, failed)) break;
                 fence_after();
-                for (int k = k_first; k < k_last; ++k, at.next()) {
+                for (int k = from_k; k < to_k; ++k, at.next()) {
                     if (!bar_wait(full(at.s), at.parity, failed)) break;
                     fence_after();
                     const uint32_t from = ring + at.s * S::stage, sf = from + S::b_bytes + S::a_bytes;
@@ -194,14 +201,67 @@ __global__ void __launch_bounds__(Shape<NT>::threads, 1)
                         const uint32_t idesc = idesc_e2m1(S::rows, NT, (q & 1) * 2), sfa = sfd + 4 * (q >> 1),
                                        sfb = sfd + 8 + 4 * S::bands * (q >> 1);
                         if constexpr (kPair)
-                            mma_e2m1_pair(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > k_first || q > 0);
+                            mma_e2m1_pair(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > from_k || q > 0);
                         else
-                            mma_e2m1(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > k_first || q > 0);
+                            mma_e2m1(d, da + 2 * q, db + 2 * q, idesc, sfa, sfb, k > from_k || q > 0);
                     }
                     commit(empty(at.s));
                 }
                 if (*failed) break;
                 commit(sum_full(done & 1));
+                from_k = LONG && to_k < k_last ? to_k : k_first;
+                if (from_k == k_first) t += stride;
+            }
+        }
+    } else if constexpr (LONG) {  // the sums of a tile are joined in registers, rounded to nearest
+        constexpr int kStep = S::writers / 4, kOwn = NT / 16 / kStep;  // this warp's chunks of 16 columns: pick, pick + kStep, ..
+        const int pick = warp / 4, quarter = warp % 4 * 32;
+        int done = 0;
+        for (int t = first; t < tiles; t += stride) {
+            float acc[kOwn * 16];
+#pragma unroll
+            for (int i = 0; i < kOwn * 16; ++i) acc[i] = 0.0f;
+            bool ok = true;
+            for (int c = 0; c < sums && ok; ++c, ++done) {
+                ok = __all_sync(~0u, bar_wait(sum_full(done & 1), (done >> 1) & 1, failed));
+                if (!ok) break;
+                fence_after();
+                const uint32_t from = tmem + (done & 1 ? S::second : 0) + (uint32_t(quarter) << 16) + pick * 16;
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) {
+                    // The columns that either sum shares first: one order for both, as two ways through here would hold
+                    // the sums twice.
+                    static_assert(kLag != 1 || (kOwn >= 4 && 2 * kStep >= 3), "they are among each warp's outer four chunks");
+                    const int own = kLag != 1 ? j : j < 2 ? j : j < 4 ? kOwn - 4 + j : j - 2;
+                    uint32_t r[16];
+                    tmem_ld16(from + kStep * own * 16, r);
+                    tmem_wait_ld(r);
+                    if (j == (kLag == 1 ? 3 : kOwn - 1)) {
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (kPair)
+                                bar_arrive_at(sum_empty(done & 1), 0);
+                            else
+                                bar_arrive(sum_empty(done & 1));
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[own * 16 + i] += __uint_as_float(r[i]);
+                }
+            }
+            if (!ok) break;
+            const int64_t row0 = int64_t(t % p.m_tiles) * NT + pick * 16;
+            const int64_t col = int64_t(t / p.m_tiles) * S::rows + half * kRows + quarter + lane;
+#pragma unroll
+            for (int own = 0; own < kOwn; ++own) {
+                if (split > 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        part_sums[((pick + kStep * own) * 16 + i) * kRows + quarter + lane] = acc[own * 16 + i];
+                } else {
+                    out.put_each(row0 + kStep * own * 16, col, [&](int i) { return acc[own * 16 + i]; });
+                }
             }
         }
     } else {
@@ -310,7 +370,6 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     Params p;
     p.a_scales = static_cast<const uint8_t *>(A.scales);
     p.b_scales = static_cast<const uint8_t *>(B.scales);
-    p.m = C.rows;
     p.steps = static_cast<int>(mx_ceil(nb, 2));
     p.scale_tiles = static_cast<int>(mx_scale_tiles(A.cols));
     p.n_tiles = static_cast<int>(mx_ceil(C.cols, S::rows));
@@ -324,7 +383,8 @@ cudaError_t launch(const costa_mx_matrix &A, const costa_mx_matrix &B, float alp
     while (!S::pair && split < kMaxSplit && tiles <= mx_clusters(2 * split, NT <= 64 ? 2 : 1) && stages_k >= 4 * split)
         split *= 2;
     const int64_t blocks = S::blocks * (split > 1 ? tiles * split : std::min<int64_t>(tiles, sms / S::blocks));
-    return mx_launch(product_kernel<NT, T>, blocks, S::threads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
+    const bool one_sum = mx_ceil(stages_k, split) <= kSumStages;
+    return mx_launch(one_sum ? product_kernel<NT, false, T> : product_kernel<NT, true, T>, blocks, S::threads, S::smem, S::blocks * split, s, a_map, b_map, a_scale_map,
                      b_scale_map, p, out, split);
 }
 

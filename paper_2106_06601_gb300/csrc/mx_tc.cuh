@@ -266,7 +266,20 @@ template <typename T> struct Output {
         if (beta != 0.0f) v += beta * to_float(*at);
         *at = from_float<T>(v);
     }
-    // The sums sum(0) .. sum(15) of 16 rows of a column.
+    // The sums sum(0) .. sum(15) of 16 rows of a column, one by one: for a caller that holds many more.
+    template <typename F> __device__ void put_each(int64_t row, int64_t col, F sum) const {
+        if (col >= cols || row >= rows) return;
+        T *at = p + row * ld + col;
+        const int n = static_cast<int>(min(int64_t(16), rows - row));
+#pragma unroll
+        for (int i = 0; i < 16; ++i, at += ld)
+            if (i < n) {
+                float v = alpha * sum(i);
+                if (beta != 0.0f) v += beta * to_float(*at);
+                *at = from_float<T>(v);
+            }
+    }
+    // The same, with what they are added to read first.
     template <typename F> __device__ void put16(int64_t row, int64_t col, F sum) const {
         if (col >= cols || row >= rows) return;
         T *at = p + row * ld + col;

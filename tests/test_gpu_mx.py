@@ -192,6 +192,37 @@ def test_product_without_columns():
     assert not C.numpy().any()
 
 
+def one_sign(rng, rows, k, repeat=1):
+    """`rows` x k codes of one sign whose blocks' scales spread over 2^8, and their values; the rows `repeat` times."""
+    codes = rng.integers(1, 8, (rows, k), np.uint8)
+    scales = (127 - rng.integers(0, 9, (rows, -(-k // 32)))).astype(np.uint8)
+    padded = np.pad(codes, ((0, 0), (0, -k % 32)))
+    q = Codes("e2m1", rows, k, packed=_mx.pack("e2m1", padded, scales, k))
+    if repeat > 1:  # whole bands of 128 rows
+        q.rows, q.codes, q.scales = rows * repeat, q.codes.repeat(repeat), q.scales.repeat(repeat)
+    unit = torch.exp2(torch.from_numpy(scales).cuda().double() - 127).repeat_interleave(32, 1)[:, :k]
+    return q, torch.from_numpy(_mx.GRID).cuda()[torch.from_numpy(codes).cuda().long()] * unit
+
+
+@pytest.mark.parametrize("m, repeat, k", [(3, 1, 2000), (3, 1, 1 << 19), (3, 160, 66000), (30, 160, 66000), (60, 160, 66000),
+                                          (120, 160, 66000), (260, 128, 66000), (260, 128, 8193), (260, 128, 8448),
+                                          (5, 3, 8200), (20, 160, 16640)])
+def test_product_sums_of_one_sign(m, repeat, k):
+    """Each product of 64 elements cuts less than 2^-23 off the growing sum, of 8192 elements at most: 64.5 units of 2^-23,
+    however large k is; then one rounding for each sum of a tile and up to 7 for the parts of k."""
+    rng = np.random.default_rng([m, k])
+    (A, a), (B, b) = one_sign(rng, m, k), one_sign(rng, 128, k, repeat)
+    n = 128 * repeat
+    for alpha, beta, kind in ((1.0, 0.0, "f32"), (0.5, 2.0, "f32"), (1.0, 0.0, "bf16")):
+        C = torch.ones(m + 1, n, device="cuda", dtype=TORCH[kind])
+        costa.costa_mx_product(A.c, B.c, costa.costa_mx_dense(kind, m, n, C.data_ptr(), n), alpha, beta, stream())
+        assert (C[m] == 1).all()
+        want = (alpha * (a @ b.t()) + beta).repeat(1, repeat)
+        units = 2 * 64.5 + k / 8192 / 2 + 7 + 3
+        off = (C[:m].double() - want).abs() / want
+        assert off.max().item() <= units * 2.0 ** -24 + (2.0 ** -8 if kind == "bf16" else 0)
+
+
 def test_product_nan_stays_in_its_rows():
     """A block of NaN reaches its own row of C and no other; so does one in B for columns."""
     rng = np.random.default_rng(3)
