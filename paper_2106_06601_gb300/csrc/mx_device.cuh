@@ -14,7 +14,8 @@ namespace mx {
 // kernel; in those that use tensor memory once they hold it: a kernel that waits
 // for this one must not hold what this one still waits for.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-// Before anything in global memory is read or written: what the kernels before this one wrote is there.
+// Before anything in global memory is read or written: what the kernels before this one wrote is there.  (A
+// product brings weights as far as the L2 cache before it, which changes nothing that a kernel sees.)
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // 2^(biased - 127) for biased in 0 .. 254; NaN for 255.

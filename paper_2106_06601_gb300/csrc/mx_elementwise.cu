@@ -589,7 +589,7 @@ template <int ACT, typename T> __device__ __forceinline__ void act_both(float x,
 
 // Y and the checkpoints from one pass over X (and G).  8192 x 16384, gated, bf16:
 // SiLU 181 us (5980 GB/s), GELU 203 us (5330), whose cdf is beside the traffic; f32:
-// 266 us (7130) and 276 us (6890).
+// 266 us (7080) and 276 us (6840).
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T> X, Dense<const T> G, Dense<T> Y, Codes QX,
                                                                Codes QG, int64_t cols, Groups gr) {
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, 4) act_forward_kernel(Dense<const T>
 
 // The gradients from the checkpoints, nothing else kept.  8192 x 16384, gated, bf16:
 // SiLU 163 us (6640 GB/s; with five blocks of an SM 171), GELU 174 us (6220); f32:
-// 272 us (6990) and 280 us (6770).
+// 272 us (6950) and 280 us (6730).
 template <typename T, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) act_backward_kernel(Codes QX, Codes QG, Dense<const T> dY, Dense<T> dX,
                                                                 Dense<T> dG, int64_t cols, Groups gr) {

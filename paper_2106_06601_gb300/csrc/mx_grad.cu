@@ -25,11 +25,13 @@
 // 8e-7 in f32.
 //
 // GB300: 4096 x 8192 x 4096 bf16 190 us (1.45 PFLOP/s, 75% of the library
-// products' rate), 16384 tokens 800 us (1.37); the same with an odd stride 470
-// us, f32 605 us (three products each: 1.36 PFLOP/s of them), f32 with an odd
-// stride 700 us.  What bounds it: the conversions' logical and bf16 operations,
-// at half rate each, and shared memory, which the operands and the converted
-// codes share, are all at 50 to 65%, and 24 warps hide no more of their latency.
+// products' rate), 16384 tokens 803 us (1.37); the same with an odd stride 476
+// us, f32 622 us (three products each: 1.33 PFLOP/s of them), f32 with an odd
+// stride 694 us.  What bounds it: the conversions' logical operations, at half
+// rate (ALU pipe 56% busy), shared memory, which the operands and the converted
+// codes share (56%; f32 59%), and the issue slots (58%; 62%): 24 or 28 warps hide
+// no more of their latency, and the tensor pipe is 64% (56%) busy.  Spilt, around
+// the roles' loops: 40 to 76 bytes a thread (f32 92).
 #include <algorithm>
 #include <type_traits>
 
@@ -432,9 +434,11 @@ struct Layout {
     double ns;
 };
 
-// The shortest by what was measured: a stage of a pair takes 375 ns with 128
-// columns of dY and 450 with 256, joining the parts some 3 and 6 us, and tiles
-// beyond what the device runs at a time take another round.  (GPU us with the
+// The shortest by what was measured with aligned bf16 dY: a stage of a pair takes
+// 375 ns with 128 columns of dY and 450 with 256, joining the parts some 3 and 6
+// us, and tiles beyond what the device runs at a time take another round.  (With
+// 128 columns of other dY a stage takes about 540, and 700 in f32; they are laid
+// out by the same figures, which weigh parts of the tokens a little too low.)  (GPU us with the
 // quantisation, 128 and 256 columns: 4096 x 2048 x 2048 55, 36; 4096 x 1024 x
 // 4096 60, 41; 512 x 4096 x 4096 32, 26; 4096 x 1024 x 1024 in two parts 21,
 // in four 32; 4096 x 512 x 512 in four 14, 17.)

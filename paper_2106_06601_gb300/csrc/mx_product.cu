@@ -12,11 +12,12 @@
 // few tiles split k over a cluster and join the parts in their order.  A long k
 // takes several sums of a tile, one after another.
 //
-// GB300: 8192 x 16384 x 8192 301 us, 7.3 PFLOP/s of a nominal 9 (products over 64
-// elements): of 784 cycles a stage the tensor cores' queue takes 621, among them
-// some 150 for copies of scales, and operands come late in 105.  1023 x 4096 x
-// 4096 10.7 us: one round of tiles, its fill and its way out.  1 x 16384 x 4096
-// 8 us for 35.6 MB of weights (4.5 TB/s): fill, and the join of two halves of k.
+// GB300: 8192 x 16384 x 8192 302 us, 7.3 PFLOP/s, where four times the measured
+// rate of library bf16 products is 7.8: the tensor pipe is 75% busy; of 784 cycles
+// a stage its queue takes 621, among them some 150 for copies of scales, and
+// operands come late in 105.  1023 x 4096 x 4096 10.7 us: one round of tiles, its
+// fill and its way out.  1 x 16384 x 4096 8.8 us for 35.6 MB of weights (4.0
+// TB/s): fill, and the join of two halves of k.
 #include <algorithm>
 
 #include "costa_internal.h"
