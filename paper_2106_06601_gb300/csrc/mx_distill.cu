@@ -716,7 +716,7 @@ cudaError_t distill(const costa_mx_dense &Z, const costa_mx_index &ids, const co
     p.tau = tau;
     const bool whole = aligned16(&Z) && aligned16(dZ) && p.cols % 8 == 0;
     if (!loss) return whole ? launch_backward<T, true>(p, s) : launch_backward<T, false>(p, s);
-    if (!dZ) return launch_loss(p, whole, s);
+    if (!dZ || p.cols == 0) return launch_loss(p, whole, s);  // (no columns: nothing of a gradient to write)
     return whole ? launch_both<T, true>(p, s) : launch_both<T, false>(p, s);
 }
 
