@@ -34,7 +34,8 @@ cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, size_t 
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024)
+    // (48 KB are granted unasked, the kernel's static shared memory among them, which is below 16 KB)
+    if (smem > 32 * 1024)
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
     if (e == cudaSuccess)

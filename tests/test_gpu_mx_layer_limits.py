@@ -3,12 +3,13 @@
 import numpy as np
 import pytest
 
+from tests import _mx_layer as ref
 
 torch = pytest.importorskip("torch")
 costa = pytest.importorskip("paper_2106_06601_gb300")
 
-from tests.test_gpu_mx import Dense, stream  # noqa: E402
-from tests.test_gpu_mx_layer import Index  # noqa: E402
+from tests.test_gpu_mx import Dense, close, matrix, stream  # noqa: E402
+from tests.test_gpu_mx_layer import Index, rounded, workspace  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +26,35 @@ def test_distill_without_columns_with_a_gradient(rows, top, dtype):
     assert not L.numpy().any()
     assert (S.numpy() == [-np.inf, 0.0]).all()
     costa.costa_mx_distill_backward(none, at.c, T.c, 1.0, S.c, G.c, none, stream())
+
+
+@pytest.mark.parametrize("n, pairs", [(372, 9000), (372, 1024), (384, 992), (384, 961), (371, 9000), (373, 9000), (385, 992), (1024, 9000)])
+def test_expert_sort_of_48_kb(n, pairs):
+    """Counts of 48 KB of shared memory, with what the kernel has besides."""
+    rng = np.random.default_rng([n, pairs])
+    e = rng.integers(0, n, (pairs, 1)).astype(np.int32)
+    E, place, starts, counts = Index(pairs, 1, e), Index(pairs, 1), Index(1, n + 1), Index(1, n)
+    costa.costa_mx_expert_sort(E.c, n, 1, place.c, starts.c, counts.c, stream())
+    for got, want in zip((place, starts, counts), ref.sort(e, n, 1)):
+        assert np.array_equal(got.numpy().reshape(want.shape), want)
+
+
+@pytest.mark.parametrize("rows, cols", [(3, 12288), (310, 12288), (305, 11265), (3, 11900), (2, 11264), (2, 12289), (4, 16384)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_norm_backward_of_48_kb(rows, cols, dtype, pad):
+    """Sums of dW of 48 KB of shared memory, with what the kernel has besides."""
+    rng = np.random.default_rng([rows, cols, pad])
+    x, dy = matrix(rng, rows, cols, dtype), matrix(rng, rows, cols, dtype)
+    w = rounded(1 + 0.1 * rng.standard_normal((1, cols)), dtype)
+    X, W, Y, S = Dense(rows, cols, dtype, x, pad), Dense(1, cols, dtype, w), Dense(rows, cols, dtype, None, pad), Dense(rows, 1, "f32")
+    costa.costa_mx_norm_forward(X.c, None, W.c, 1e-5, None, Y.c, S=S.c, stream=stream())
+    dY, dX, dW, work = Dense(rows, cols, dtype, dy, pad), Dense(rows, cols, dtype, None, pad), Dense(1, cols, "f32"), workspace(rows, cols)
+    costa.costa_mx_norm_backward(dY.c, X.c, S.c, W.c, None, dX.c, dW.c, work.data_ptr(), work.numel() - 32, stream())
+    h, w, dy = x.astype(np.float64), w.astype(np.float64), dy.astype(np.float64)
+    y, s = ref.norm(h, w, np.float64(np.float32(1e-5)))
+    close(Y.numpy(), y, ref.norm_tol(y, dtype))
+    dx, dw, mean = ref.norm_grad(dy, h, s, w)
+    tol_x, tol_w = ref.norm_grad_tol(dx, dw, dy, h, s, w, np.zeros_like(h), mean, dtype, "f32", rows)
+    close(dX.numpy(), dx, tol_x)
+    close(dW.numpy(), dw, tol_w)
