@@ -481,7 +481,7 @@ cudaError_t launch_mx_expert_sort(const costa_mx_index &experts, int n_experts, 
                                                                 mx_ceil(n_experts, 32)));
     const int blocks = many ? mx::kSortBlocks : 1;
     p.per_warp = mx_ceil(mx_ceil(p.pairs, int64_t(blocks) * warps), 32) * 32;
-    const size_t smem = sizeof(int) * (size_t(warps) + 1) * n_experts;
+    const MxShared smem(sizeof(int) * (size_t(warps) + 1) * n_experts, sizeof(int) * (mx::kSortThreads / 32 + 1) * COSTA_MX_MAX_EXPERTS);
     return many ? mx_launch(mx::sort_kernel<mx::kSortBlocks>, blocks, 32 * warps, smem, blocks, s, p)
                 : mx_launch(mx::sort_kernel<1>, blocks, 32 * warps, smem, 1, s, p);
 }

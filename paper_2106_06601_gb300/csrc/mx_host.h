@@ -11,6 +11,16 @@
 
 namespace costa {
 
+// Dynamic shared memory of a launch, and the most that any launch of its kernel
+// takes.  A kernel is always allowed the latter: what it is allowed is one number
+// for all host threads, and a thread that lowered it between another's asking and
+// launching would have that launch refused.
+struct MxShared {
+    size_t bytes, most;
+    MxShared(size_t always) : bytes(always), most(always) {}
+    MxShared(size_t bytes_, size_t most_) : bytes(bytes_), most(most_) {}
+};
+
 // Launches a kernel of the low-bit operators, in clusters of `cluster` blocks,
 // as a dependent of the kernel before it on the stream: its blocks may start
 // when that one's have all started (or, for a kernel that says nothing, ended),
@@ -18,13 +28,13 @@ namespace costa {
 // writes are visible.  Measured on GB300, two launches that follow each other
 // (a token's quantisation and its inverse): 3.9 -> 2.4 us each.
 template <typename... P, typename... A>
-cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, size_t smem, int cluster, cudaStream_t s,
+cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, MxShared smem, int cluster, cudaStream_t s,
                       A &&...args) {
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = smem.bytes;
     cfg.stream = s;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -35,8 +45,8 @@ cudaError_t mx_launch(void (*kernel)(P...), int64_t blocks, int threads, size_t 
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     cudaError_t e = cudaSuccess;
     // (48 KB are granted unasked, the kernel's static shared memory among them, which is below 16 KB)
-    if (smem > 32 * 1024)
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (smem.bytes > 32 * 1024)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem.most));
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
     if (e == cudaSuccess)
         count_launch();

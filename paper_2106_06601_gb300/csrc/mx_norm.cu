@@ -710,14 +710,14 @@ template <typename T> int window_threads(int64_t cols) {
 // Blocks to an SM and rows under way in each (two at least), for rows of `arrays` matrices.
 struct Under {
     int blocks, stages;
-    size_t bytes;
+    MxShared bytes;
 };
 Under under_way(int threads, int arrays, int size, int most_blocks) {
     const size_t stage = size_t(16) * arrays * (kStreamGroups * (size / 2) * threads + 2);  // (windows need two pieces more)
     int blocks = std::max(1, std::min(most_blocks, 1024 / threads));
     while (blocks > 1 && kStreamBytes / (blocks * stage) < 3) --blocks;
     const int stages = static_cast<int>(std::min<size_t>(4, kStreamBytes / (blocks * stage)));
-    return {blocks, stages, stage * stages};
+    return {blocks, stages, MxShared(stage * stages, kStreamBytes)};
 }
 static_assert(kStreamBytes / (16 * 3 * (kStreamGroups * 2 * kStreamThreads + 2)) >= 2, "two rows of the widest");
 
@@ -793,7 +793,8 @@ cudaError_t backward(const costa_mx_dense &dY, const costa_mx_dense &H, const co
         e = with_shape<kBackwardMost>(shape, aligned, [&](auto c, auto most, auto line) {
             constexpr int C = decltype(c)::value, kMost = decltype(most)::value;
             const int threads = kMost == 32 ? 32 * kWarps : shape.threads;
-            const size_t wide = kMost == 32 || C < 4 ? 0 : sizeof(float) * 8 * C * threads;
+            constexpr size_t kWide = kMost == 32 || C < 4 ? 0 : sizeof(float) * 8 * C;  // of a thread
+            const MxShared wide(kWide * threads, kWide * kMost);
             parts = std::min<int64_t>(kMost == 32 ? mx_ceil(H.rows, kWarps) : H.rows, mx_norm_parts(H.cols));
             return mx_launch(norm_backward_kernel<T, C, kMost, decltype(line)::value>, parts, threads, wide, 1, s, p);
         });

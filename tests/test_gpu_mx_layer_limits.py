@@ -1,4 +1,5 @@
 """Norm, experts' rows and distillation at the limits of what their calls take, and where their kernels change."""
+import threading
 
 import numpy as np
 import pytest
@@ -58,3 +59,57 @@ def test_norm_backward_of_48_kb(rows, cols, dtype, pad):
     tol_x, tol_w = ref.norm_grad_tol(dx, dw, dy, h, s, w, np.zeros_like(h), mean, dtype, "f32", rows)
     close(dX.numpy(), dx, tol_x)
     close(dW.numpy(), dw, tol_w)
+
+
+def test_calls_of_unlike_sizes_from_several_threads():
+    """Host threads whose calls need shared memory of unlike sizes of the same kernels, each on its own stream and storage,
+    do not refuse each other's."""
+    rng = np.random.default_rng(3)
+
+    class Job:
+        def __init__(self, rows, cols, n):
+            self.stream, self.failed = torch.cuda.Stream(), []
+            x, e = matrix(rng, rows, cols, "bf16"), rng.integers(0, n, (1030, 1)).astype(np.int32)
+            X, Y, dX, W = Dense(rows, cols, "bf16", x), Dense(rows, cols, "bf16"), Dense(rows, cols, "bf16"), Dense(1, cols, "bf16", np.ones((1, cols)))
+            S, dW, work = Dense(rows, 1, "f32"), Dense(1, cols, "f32"), workspace(rows, cols)
+            E, place, starts, counts = Index(1030, 1, e), Index(1030, 1), Index(1, n + 1), Index(1, n)
+            self.kept, self.outputs = (X, W, E, work), (Y, S, dX, dW, place, starts, counts)
+            st = self.stream.cuda_stream
+            # (arguments made once: Python's lock is held while they are, and calls would hardly meet)
+            self.calls = [
+                (costa.costa_mx_norm_forward, (X.c, None, W.c, 1e-5, None, Y.c, None, None, S.c, st)),
+                (costa.costa_mx_norm_backward, (Y.c, X.c, S.c, W.c, None, dX.c, dW.c, work.data_ptr(), work.numel() - 32, st)),
+                (costa.costa_mx_expert_sort, (E.c, n, 1, place.c, starts.c, counts.c, st))]
+
+        def many(self, start, times):
+            start.wait()
+            try:
+                for _ in range(times):
+                    for call, args in self.calls:
+                        call(*args)
+            except costa.CostaError as err:
+                self.failed.append(str(err))
+
+        def results(self):
+            return [v.numpy() for v in self.outputs]
+
+    # rows through shared memory as they lie and as windows, sums of dW there; and sorts by some more experts
+    jobs = [Job(*sizes) for sizes in ((310, 3000, 400), (305, 6144, 1024), (310, 2777, 500), (312, 6001, 800), (1, 12800, 450), (1, 30000, 700))]
+    torch.cuda.synchronize()
+    alone = []
+    for job in jobs:
+        job.many(threading.Barrier(1), 1)
+        torch.cuda.synchronize()
+        assert not job.failed
+        alone.append(job.results())
+    start = threading.Barrier(len(jobs))
+    threads = [threading.Thread(target=job.many, args=(start, 3000)) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not [job.failed for job in jobs if job.failed]
+    for job, want in zip(jobs, alone):
+        for a, b in zip(job.results(), want):
+            assert np.array_equal(a, b)
