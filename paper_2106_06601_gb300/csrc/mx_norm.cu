@@ -22,9 +22,10 @@ namespace {
 
 constexpr int kWarps = 4;  // of a block whose warps take a row each
 
-// 1 / sqrt(sum / n + eps), or where the sum of squares left f32's range the same from one of elements 2^-100 times as
-// large: above 2^128 / n the largest element is above 2^48, so what is lost below does not count; eps does not either.
-__device__ __forceinline__ float inverse_root(float sum, float n, float eps) { return __frsqrt_rn(__fdiv_rn(sum, n) + eps); }
+// s = 1 / sqrt(sum / n + eps); or where the sum of squares, or that sum, left f32's range, kDown times the same of elements
+// kDown = 2^-100 times as large and of kDown^2 eps: the largest element is above 2^56 then (there are 2^15 at most), beside
+// which what underflows does not count.
+__device__ __forceinline__ float square(float sum, float n, float eps) { return __fdiv_rn(sum, n) + eps; }
 constexpr float kDown = 7.888609052210118e-31f;  // 2^-100
 
 // A kernel's MOST: the most threads that share a row; a warp's 32 have a block of kWarps rows.
@@ -130,15 +131,15 @@ __global__ void __launch_bounds__(threads_of(MOST)) norm_forward_kernel(const Fo
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(h[j](i), h[j](i), sum);
     const float n = static_cast<float>(p.cols);
-    sum = row_sum<WARP>(sum, sums, 0);
-    float s = inverse_root(sum, n, p.eps);
-    if (sum == INFINITY) {
+    const float all = square(row_sum<WARP>(sum, sums, 0), n, p.eps);
+    float s = __frsqrt_rn(all);
+    if (all == INFINITY) {
         sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < C; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(h[j](i) * kDown, h[j](i) * kDown, sum);
-        s = kDown * inverse_root(row_sum<WARP>(sum, sums, 1), n, 0.0f);
+        s = kDown * __frsqrt_rn(square(row_sum<WARP>(sum, sums, 1), n, p.eps * kDown * kDown));
     }
     if (p.s && first == 0) p.s[row * p.lds] = s;
 #pragma unroll
@@ -405,15 +406,15 @@ template <typename T, bool WHOLE> __global__ void __launch_bounds__(kStreamThrea
             for (int i = 0; i < 8; ++i) sum = fmaf(h[j](i), h[j](i), sum);
         }
         stage = stage + 1 == stages ? 0 : stage + 1;
-        sum = row_sum<false>(sum, sums, turn);
-        float s = inverse_root(sum, n, p.eps);
-        if (sum == INFINITY) {
+        const float all = square(row_sum<false>(sum, sums, turn), n, p.eps);
+        float s = __frsqrt_rn(all);
+        if (all == INFINITY) {
             sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < C; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[j](i) * kDown, h[j](i) * kDown, sum);
-            s = kDown * inverse_root(row_sum<false>(sum, sums, 2), n, 0.0f);
+            s = kDown * __frsqrt_rn(square(row_sum<false>(sum, sums, 2), n, p.eps * kDown * kDown));
         }
         if (p.s && first == 0) p.s[row * p.lds] = s;
 #pragma unroll

@@ -113,3 +113,31 @@ def test_calls_of_unlike_sizes_from_several_threads():
     for job, want in zip(jobs, alone):
         for a, b in zip(job.results(), want):
             assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("rows, cols", [(3, 1), (2, 2), (9, 33), (5, 600), (3, 4100), (310, 1200), (310, 1203), (3, 9000)])
+@pytest.mark.parametrize("eps", [2.0 ** 127, 2.0 ** 126, 2.0 ** 100, 2.0 ** 90, 1e-6])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("res", [False, True])
+def test_norm_of_a_large_eps(rows, cols, eps, dtype, res):
+    """An eps of any size counts also where the squares, their sum or it and their mean leave f32's range."""
+    rng = np.random.default_rng([rows, cols])
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(50, 64, (rows, 1)))
+    x[0], x[1] = 2.0 ** 64, 1.875 * 2.0 ** 63  # of one column the mean leaves the range; it and eps do
+    x = rounded(x, dtype)
+    eps = np.float32(eps)
+    W, w = Dense(1, cols, "f32", np.full((1, cols), 2.0 ** 40)), np.full((1, cols), 2.0 ** 40)
+    X, Y, S, H = Dense(rows, cols, dtype, x), Dense(rows, cols, dtype), Dense(rows, 1, "f32"), Dense(rows, cols, dtype)
+    R = Dense(rows, cols, dtype, np.zeros((rows, cols)))
+    costa.costa_mx_norm_forward(X.c, R.c if res else None, W.c, eps, H.c if res else None, Y.c, S=S.c, stream=stream())
+    h = x.astype(np.float64)
+    y, s = ref.norm(h, w, np.float64(eps))
+    close(S.numpy(), s, 1.01 * ref.S_UNITS * ref.U * s)
+    close(Y.numpy(), y, ref.norm_tol(y, dtype))
+    dy = rounded(rng.standard_normal((rows, cols)), dtype)
+    dY, dX, dW, work = Dense(rows, cols, dtype, dy), Dense(rows, cols, dtype), Dense(1, cols, "f32"), workspace(rows, cols)
+    costa.costa_mx_norm_backward(dY.c, X.c, S.c, W.c, None, dX.c, dW.c, work.data_ptr(), work.numel() - 32, stream())
+    dx, dw, mean = ref.norm_grad(dy.astype(np.float64), h, s, w)
+    tol_x, tol_w = ref.norm_grad_tol(dx, dw, dy.astype(np.float64), h, s, w, np.zeros_like(h), mean, dtype, "f32", rows)
+    close(dX.numpy(), dx, tol_x)
+    close(dW.numpy(), dw, tol_w)
