@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 costa = pytest.importorskip("paper_2106_06601_gb300")
 
 from tests.test_gpu_mx import Dense, close, matrix, stream  # noqa: E402
-from tests.test_gpu_mx_layer import Index, rounded, workspace  # noqa: E402
+from tests.test_gpu_mx_layer import Index, places, rounded, workspace  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -141,3 +141,22 @@ def test_norm_of_a_large_eps(rows, cols, eps, dtype, res):
     tol_x, tol_w = ref.norm_grad_tol(dx, dw, dy.astype(np.float64), h, s, w, np.zeros_like(h), mean, dtype, "f32", rows)
     close(dX.numpy(), dx, tol_x)
     close(dW.numpy(), dw, tol_w)
+
+
+@pytest.mark.parametrize("tokens, cols, top, rows", [(3, 33, 2, 9), (50, 900, 3, 200), (130, 1027, 8, 1200), (64, 4096, 9, 700), (9, 2777, 33, 300)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad, pad_dz", [(0, 0), (3, 3), (8, 1), (1, 8)])
+def test_weights_gradient_by_itself_and_over_z(tokens, cols, top, rows, dtype, pad, pad_dz):
+    """dweights is added up in one order, whatever else is written: its bits are the same with dZ beside it, alone, and with
+    dZ over Z, which a read of Z after its overwriting would change."""
+    rng = np.random.default_rng([tokens, cols, pad])
+    at = places(rng, tokens, top, rows)
+    z, dy = matrix(rng, rows, cols, dtype), matrix(rng, tokens, cols, dtype)
+    Z, dY = Dense(rows, cols, dtype, z, pad), Dense(tokens, cols, dtype, dy, pad)
+    place, W = Index(tokens, top, at), Dense(tokens, top, "f32", rng.standard_normal((tokens, top)).astype(np.float32))
+    beside, alone, over = (Dense(tokens, top, "f32") for _ in range(3))
+    costa.costa_mx_combine_backward(dY.c, Z.c, place.c, W.c, Dense(rows, cols, dtype, None, pad_dz).c, None, beside.c, stream())
+    costa.costa_mx_combine_backward(dY.c, Z.c, place.c, W.c, None, None, alone.c, stream())
+    costa.costa_mx_combine_backward(dY.c, Z.c, place.c, W.c, Z.c, None, over.c, stream())
+    assert np.array_equal(alone.numpy(), beside.numpy())
+    assert np.array_equal(over.numpy(), beside.numpy())
