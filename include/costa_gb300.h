@@ -839,7 +839,9 @@ costa_status costa_mx_norm_backward(const costa_mx_dense *dY, const costa_mx_den
  * of each expert, a multiple of `align`, and where the last one's ends, rounded up
  * to one; counts (1 x n_experts): its rows.  Rows of codes in E2M1 that are to be
  * an expert's matrix by themselves need align = 128 (a band of their scales).  The
- * sorted rows span tokens * k + n_experts * (align - 1) at most.
+ * sorted rows span tokens * k + n_experts * (align - 1) at most.  Products take an
+ * expert's extents from the host: a program that runs one for each expert reads
+ * starts and counts back after the sort, which a graph cannot hold.
  * Errors: INVALID_ARG, SHAPE, LAYOUT, CUDA. */
 costa_status costa_mx_expert_sort(const costa_mx_index *experts, int32_t n_experts, int32_t align,
                                   const costa_mx_index *place, const costa_mx_index *starts,
@@ -848,7 +850,8 @@ costa_status costa_mx_expert_sort(const costa_mx_index *experts, int32_t n_exper
 /* Row i of X to row place(i, s) of Y and / or, as codes, of Q4 (E2M1) and Q8 (I8),
  * for every s.  Places below 0 or past the outputs' rows are left out; no two of
  * them are the same; other rows are left as they are.  Of Y (X's type), Q4 and Q8
- * any may be NULL, but one; they have the same number of rows.
+ * any may be NULL, but one; they have the same number of rows.  X is dense: a norm
+ * before it writes Y, and the codes are made here.
  * Errors: INVALID_ARG, SHAPE, DTYPE, LAYOUT, CUDA. */
 costa_status costa_mx_dispatch(const costa_mx_dense *X, const costa_mx_index *place, const costa_mx_dense *Y,
                                const costa_mx_matrix *Q4, const costa_mx_matrix *Q8, void *stream);
@@ -863,8 +866,8 @@ costa_status costa_mx_combine(const costa_mx_dense *Z, const costa_mx_index *pla
 
 /* The gradients of costa_mx_combine: row place(i, s) of dZ, and / or its codes Q4
  * (E2M1), = weights(i, s) times row i of dY; dweights(i, s) = <row place(i, s) of
- * Z, row i of dY>, 0 where the place is left out.  Other rows of dZ are left as
- * they are.  dZ and Q4 may be NULL; Z and dweights (f32) are both given or both
+ * Z, row i of dY>, 0 where the place is left out.  Where dZ or Q4 is given no two
+ * places are the same; other rows of them are left as they are.  dZ and Q4 may be NULL; Z and dweights (f32) are both given or both
  * NULL; one output at least is given.  dY, Z and dZ have one type; dZ may be Z.
  * Errors: INVALID_ARG, SHAPE, DTYPE, LAYOUT, CUDA. */
 costa_status costa_mx_combine_backward(const costa_mx_dense *dY, const costa_mx_dense *Z, const costa_mx_index *place,
@@ -880,6 +883,7 @@ costa_status costa_mx_combine_backward(const costa_mx_dense *dY, const costa_mx_
  * one column: their p add up.  One label to a row (k = 1, tau = 1) gives the cross
  * entropy.  Logits of -infinity have q = 0; an entry whose p underflows counts
  * nothing; a row that names some, but whose own logits are all -infinity, is NaN.
+ * Distances of finite logits beyond f32's range count as infinite.
  * loss: rows x 1, f32.  stats (rows x 2, f32): the row's largest logit
  * and the sum of exp((z - largest) / tau).  G (rows x 1, f32) and dZ (Z's type) are
  * both given, for dZ = G_i tau (q - p) in the same pass, or both NULL.  dZ may be Z.

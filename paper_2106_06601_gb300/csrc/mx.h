@@ -36,7 +36,7 @@ cudaError_t launch_mx_product(const costa_mx_matrix &A, const costa_mx_matrix &B
 cudaError_t launch_mx_weight_grad(const costa_mx_dense &dY, const costa_mx_matrix &QX, float alpha, float beta,
                                   const costa_mx_dense &dW, cudaStream_t s);
 
-// Blocks of the norm's gradients, each with partial sums of dW: four to an SM where a warp takes a row, else two.
+// Blocks of the norm's gradients at most, each with partial sums of dW: four to an SM up to 1024 columns, else two.
 constexpr int64_t mx_norm_parts(int64_t cols) { return cols <= 1024 ? 608 : 304; }
 // R with H may be null; and any of Y, Q4, Q8 and S.
 cudaError_t launch_mx_norm_forward(const costa_mx_dense &X, const costa_mx_dense *R, const costa_mx_dense &W, float eps,

@@ -4,12 +4,16 @@
 //   dx_ij = s_i (g_ij - u_ij c_i) + dh_ij  with  u = h s, g = dy w, c_i = mean_j g_ij u_ij
 //   dw_j = sum_i dy_ij u_ij
 //
-// Every matrix is read and written once, so memory bounds large calls, and the
-// latency of one row small ones.  A row stays in the registers of a warp (up to
-// 1024 elements) or of a thread block between its sum and what is written.
+// Memory bounds large calls, and the latency of one row small ones.  A row stays in
+// the registers of a warp (up to 1024 elements, of the gradients 512) or of a thread
+// block between its sum and what is written; only the gradients of more than 8192
+// columns read dY and H twice.
 // GB300, 8192 x 8192 bf16: the norm 92 us (5.8 TB/s, X and R read, H and Y written),
-// its gradients 84 us (6.4 TB/s with the join of dW); as 4- and 8-bit codes 2047 x
-// 8192 take 28 us, which 41 instructions an element bound.  One row of 4096: 2 us.
+// its gradients 84 us (6.4 TB/s with the join of dW).  As 4- and 8-bit codes 2047 x
+// 8192 take 28 us (floor 18.7): 41 instructions an element in 69% of the issue slots,
+// between waits for the row's other warps; 100 bytes a thread are spilled at the 64
+// registers that let two blocks share an SM.  4096 x 16384: 80 us (floor 79), gradients
+// 138 (floor 79).  One row of 4096: 2 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -708,7 +712,9 @@ Shape shape_of(int64_t cols, int64_t rows, int most) {
 template <typename T> int window_threads(int64_t cols) {
     return static_cast<int>(mx_ceil(mx_ceil(cols + 16 / sizeof(T), 8 * kStreamGroups), 32) * 32);
 }
-// Blocks to an SM and rows under way in each (two at least), for rows of `arrays` matrices.
+// Blocks to an SM and rows under way in each (two at least), for rows of `arrays` matrices, by shared memory and 1024 threads.
+// (The gradients' 128 registers leave room for 512 threads: of two blocks of more than 256 each the second then waits for the
+// first; 8192 x 5120 bf16 68 us, floor 49, where 4096 columns take 47, floor 40.)
 struct Under {
     int blocks, stages;
     MxShared bytes;
